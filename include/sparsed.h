@@ -62,6 +62,12 @@ typedef enum sparsed_status {
 #define SPARSED_OP_PATTERN_VALIDATE 4
 #define SPARSED_OP_SELECT_POOLED_QK 5
 #define SPARSED_OP_ATTENTION_STEP 6
+#define SPARSED_OP_ATTN_PACKED 7
+#define SPARSED_OP_CACHE_WRITE 8
+
+/* Types of the packed and the paged calls' tensors (the other calls take bf16). */
+#define SPARSED_DTYPE_BF16 0
+#define SPARSED_DTYPE_FP16 1
 
 /* Schedule modes returned by sparsed_schedule_mode. */
 #define SPARSED_MODE_FULL 0
@@ -288,11 +294,103 @@ sparsed_status sparsed_build_window_pattern(int32_t batch, int32_t heads_q, int3
 sparsed_status sparsed_pattern_validate(const sparsed_pattern *pattern, void *ws, size_t ws_bytes,
                                         void *cuda_stream);
 
+/*
+ * Attention over packed sequences of different lengths, with or without a causal mask. Sequence b's query rows are rows
+ * [cu_q[b], cu_q[b+1]) of q and o, its keys and values rows [cu_k[b], cu_k[b+1]) of k and v. With len_q and len_k of them,
+ * row i of a sequence sees every key of it (causal = 0), or its keys j <= i + len_k - len_q (causal = 1: the queries are
+ * the sequence's last tokens; len_k > len_q continues cached text).
+ *   O_i = sum_j p_ij V_j over the seen keys, p = softmax(softmax_scale * Q K^T); a row that sees no key gets O = 0 and
+ *   LSE = -inf. What a row does not see does not reach it, whatever its bits are (NaN and infinities included).
+ * q, o: device [total_q, heads_q, 128], k, v: device [total_k, heads_kv, 128], bf16 or fp16 (`dtype`), strides (token, head)
+ * in elements, all-zero = contiguous. cu_q, cu_k: device int32 [num_seqs + 1], ascending from 0; rows from cu_q[num_seqs] on
+ * are left as they were. lse_or_null: device fp32 [heads_q, total_q], natural log. A sequence may be empty on either side.
+ * Offsets that descend or leave [0, total] are clipped, never followed, and recorded as device status 6.
+ * Workspace: SPARSED_STATUS_BYTES. Errors: INVALID_ARG, UNSUPPORTED (head_dim != 128, dtype), ALIGNMENT, WORKSPACE, ARCH, CUDA.
+ */
+typedef struct sparsed_packed {
+  int32_t num_seqs, total_q, total_k, heads_q, heads_kv, head_dim;
+  int32_t dtype;  /* SPARSED_DTYPE_* */
+  int32_t causal; /* 0 or 1 */
+  int64_t q_strides[2], k_strides[2], v_strides[2], o_strides[2]; /* elements: token, head */
+  float softmax_scale;                                            /* 0 => 1/sqrt(head_dim) */
+} sparsed_packed;
+
+sparsed_status sparsed_attn_packed(const sparsed_packed *shape, const int32_t *cu_q, const int32_t *cu_k, const void *q,
+                                   const void *k, const void *v, void *o, float *lse_or_null, void *ws, size_t ws_bytes,
+                                   void *cuda_stream);
+
+/*
+ * A paged key-value cache. Position j of sequence b lies in page page_table[b][j / page_size] of the pools k and v
+ * ([num_pages, page_size, heads_kv, 128] by default; any strides), at place j % page_size. Only the first
+ * ceil(seq_lens[b] / page_size) entries of a table row are read. Sequences may share pages that are only read.
+ * A table entry outside [0, num_pages) that is needed, or a length beyond max_pages * page_size, is not followed: its
+ * positions are treated as absent and device status 5 is recorded. Negative lengths count as 0.
+ * page_size: 16, 32, 64, 128 or 256. Strides are multiples of 8 elements, all-zero strides mean contiguous.
+ */
+typedef struct sparsed_cache {
+  void *k, *v;               /* device */
+  const int32_t *page_table; /* device [batch, max_pages], rows table_stride entries apart (0: max_pages) */
+  int32_t *seq_lens;         /* device [batch]; written only as the `to` of sparsed_cache_evict */
+  int64_t table_stride;
+  int64_t k_strides[3], v_strides[3]; /* elements: page, place in page, head */
+  int32_t num_pages, page_size, heads_kv, head_dim, batch, max_pages;
+  int32_t dtype; /* SPARSED_DTYPE_* */
+} sparsed_cache;
+
+/*
+ * Writes the keys and values of new tokens into a cache. seq_lens counts the new tokens already: the n_b = cu_new[b+1] -
+ * cu_new[b] tokens of sequence b go to its last n_b positions, seq_lens[b] - n_b onwards. k_new, v_new: device
+ * [total_new, heads_kv, 128] of the cache's type, strides (token, head); cu_new: device int32 [batch + 1], ascending from 0;
+ * tokens from cu_new[batch] on are ignored, and so are tokens whose position is negative or has no page (status 5). Two
+ * sequences must not write to the same place. Workspace: SPARSED_STATUS_BYTES.
+ */
+sparsed_status sparsed_cache_write(const sparsed_cache *cache, const void *k_new, const int64_t k_new_strides[2],
+                                   const void *v_new, const int64_t v_new_strides[2], const int32_t *cu_new,
+                                   int32_t total_new, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * Attention of one new token per sequence over its cached keys (the token's own among them, once written):
+ *   o[b,h] = sum_j p_hj V_j, j < seq_lens[b], p_h = softmax(softmax_scale * q[b,h] K^T).
+ * q, o: device [batch, heads_q, 128] of the cache's type, strides (sequence, head), all-zero = contiguous. lse_or_null:
+ * device fp32 [batch, heads_q], natural log. An empty sequence gets zeros and -inf.
+ * mass_out_or_null: device fp32 [batch, heads_kv, mass_capacity], mass_capacity >= max_pages * page_size: receives, for
+ * j < seq_lens[b], mass_in[b,g,j] (0 without mass_in) + the sum of p_hj over the query heads h of key-value head g; what lies
+ * behind a sequence's length is left as it was. mass_in may be mass_out itself. The work is divided over the device by the
+ * lengths found in seq_lens, so a sequence's result may differ in its last bits with what else is in the batch; the same
+ * inputs give the same bits.
+ * Workspace: sparsed_paged_workspace_bytes(cache, heads_q, with_mass) bytes (with_mass: mass_out is given).
+ */
+sparsed_status sparsed_paged_workspace_bytes(const sparsed_cache *cache, int32_t heads_q, int32_t with_mass,
+                                             size_t *out_bytes); /* host only */
+sparsed_status sparsed_attn_paged(const sparsed_cache *cache, int32_t heads_q, const void *q, const int64_t q_strides[2],
+                                  void *o, const int64_t o_strides[2], float softmax_scale, float *lse_or_null,
+                                  const float *mass_in_or_null, float *mass_out_or_null, int64_t mass_capacity, void *ws,
+                                  size_t ws_bytes, void *cuda_stream);
+
+/*
+ * Eviction by accumulated attention weight: of every sequence and key-value head of `from`, min(keep, length) keys move to
+ * the first positions of `to`, in their order. With length <= keep those are all; otherwise the last `recent` ones and, of
+ * the others, the keep - recent with the largest mass (ties, +0 and -0 among them, to the lower position; NaN ranks lowest).
+ * Different heads keep different keys of a sequence. `to` has the batch, heads and type of `from`; its pages (of any
+ * supported size, of the same pool or another) must not be pages that `from` reads, and its seq_lens, which the call writes,
+ * not those of `from`. keep <= to->max_pages * to->page_size, 0 <= recent <= keep, keep >= 1.
+ * mass: device fp32 [batch, heads_kv, mass_capacity], mass_capacity >= from's max_pages * page_size. mass_out: device fp32
+ * [batch, heads_kv, mass_out_capacity], mass_out_capacity >= keep: the kept keys' mass, then zeros to the row's end.
+ * kept: device int32 [batch, heads_kv, keep]: the kept positions, ascending, -1 behind the last.
+ * A kept key whose page does not exist comes over as zeros; one whose new page does not exist is dropped (status 5).
+ * Workspace: sparsed_evict_workspace_bytes(from) bytes.
+ */
+sparsed_status sparsed_evict_workspace_bytes(const sparsed_cache *from, size_t *out_bytes); /* host only */
+sparsed_status sparsed_cache_evict(const sparsed_cache *from, const float *mass, int64_t mass_capacity, int32_t keep,
+                                   int32_t recent, const sparsed_cache *to, float *mass_out, int64_t mass_out_capacity,
+                                   int32_t *kept, void *ws, size_t ws_bytes, void *cuda_stream);
+
 /* Reads the device status word (synchronises the stream). code 0 = fine, 1 = a bounded wait ran out
  * (`where` identifies the wait), 2 = a kernel found its shared memory misaligned, 3 = sparsed_attn_sparse
  * met a row_ptr entry that points outside col_idx (that query block's rows were written as zeros),
  * 4 = the two CTAs of a pair in sparsed_attn_full_stats got different tensor-memory bases (the pair did no
- * work). Returns SPARSED_ERR_DEVICE_TIMEOUT if code != 0. */
+ * work), 5 = a page-table entry or a length of a paged cache that points outside it (see sparsed_cache), 6 = offsets of
+ * packed sequences that descend or leave the tensor. Returns SPARSED_ERR_DEVICE_TIMEOUT if code != 0. */
 sparsed_status sparsed_last_device_status(void *ws, void *cuda_stream, int32_t *code, int32_t *where);
 
 /*

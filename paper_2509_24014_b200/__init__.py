@@ -8,4 +8,6 @@ from .binding import (  # noqa: F401
     sparsed_kept_per_row, sparsed_last_device_status, sparsed_pattern_validate, sparsed_schedule_mode,
     sparsed_select_from_scores, sparsed_select_pattern, sparsed_select_pattern_pooled_qk, sparsed_select_pattern_static, sparsed_switch_step, sparsed_workspace_bytes,
     sparsed_workspace_init, sparsed_selftest_wait_timeout, save_pattern, load_pattern,
+    DTYPE_BF16, DTYPE_FP16, OP_ATTN_PACKED, OP_CACHE_WRITE, Cache, Packed, make_cache, sparsed_attn_packed, sparsed_attn_paged,
+    sparsed_cache_evict, sparsed_cache_write, sparsed_evict_workspace_bytes, sparsed_paged_workspace_bytes,
 )

@@ -17,7 +17,8 @@ from . import build as _build
 
 STATUS_BYTES = 256
 (OP_ATTN_FULL, OP_SELECT_PATTERN, OP_SELECT_FROM_SCORES, OP_ATTN_SPARSE, OP_PATTERN_VALIDATE, OP_SELECT_POOLED_QK,
- OP_ATTENTION_STEP) = range(7)
+ OP_ATTENTION_STEP, OP_ATTN_PACKED, OP_CACHE_WRITE) = range(9)
+DTYPE_BF16, DTYPE_FP16 = 0, 1
 MODE_FULL, MODE_FULL_AND_SELECT, MODE_SPARSE = 0, 1, 2
 VARIANT_NO_REUSE, VARIANT_NO_ISOLATION = 1, 2
 
@@ -28,7 +29,8 @@ EXPORTED_SYMBOLS = (
     "sparsed_status_string", "sparsed_last_cuda_error", "sparsed_select_pattern_static",
     "sparsed_tile_stats_bytes", "sparsed_attn_full_stats", "sparsed_select_from_stats",
     "sparsed_build_window_pattern", "sparsed_selftest_wait_timeout", "sparsed_select_pattern_pooled_qk",
-    "sparsed_attention_step", "sparsed_attention_step_variant",
+    "sparsed_attention_step", "sparsed_attention_step_variant", "sparsed_attn_packed", "sparsed_cache_write",
+    "sparsed_paged_workspace_bytes", "sparsed_attn_paged", "sparsed_evict_workspace_bytes", "sparsed_cache_evict",
 )
 
 
@@ -56,6 +58,23 @@ class Pattern(ctypes.Structure):
     _fields_ = [("row_ptr", ctypes.c_void_p), ("col_idx", ctypes.c_void_p), ("col_capacity", ctypes.c_int64),
                 ("nnz", ctypes.c_int64), ("block_size", ctypes.c_int32), ("num_blocks", ctypes.c_int32),
                 ("batch", ctypes.c_int32), ("heads_q", ctypes.c_int32)]
+
+
+class Packed(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("total_q", ctypes.c_int32), ("total_k", ctypes.c_int32),
+                ("heads_q", ctypes.c_int32), ("heads_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("causal", ctypes.c_int32), ("q_strides", ctypes.c_int64 * 2),
+                ("k_strides", ctypes.c_int64 * 2), ("v_strides", ctypes.c_int64 * 2), ("o_strides", ctypes.c_int64 * 2),
+                ("softmax_scale", ctypes.c_float)]
+
+
+class Cache(ctypes.Structure):
+    """sparsed_cache. The object keeps its tensors (`tensors`: k, v, page_table, seq_lens) alive."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("seq_lens", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("k_strides", ctypes.c_int64 * 3),
+                ("v_strides", ctypes.c_int64 * 3), ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("heads_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("batch", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 _lib = None
@@ -99,6 +118,13 @@ def load_library() -> ctypes.CDLL:
     lib.sparsed_workspace_init.argtypes = [vp, sz, vp]
     lib.sparsed_pattern_validate.argtypes = [P(Pattern), vp, sz, vp]
     lib.sparsed_last_device_status.argtypes = [vp, vp, P(i32), P(i32)]
+    i64, f32 = ctypes.c_int64, ctypes.c_float
+    lib.sparsed_attn_packed.argtypes = [P(Packed), vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.sparsed_cache_write.argtypes = [P(Cache), vp, P(i64), vp, P(i64), vp, i32, vp, sz, vp]
+    lib.sparsed_paged_workspace_bytes.argtypes = [P(Cache), i32, i32, P(sz)]
+    lib.sparsed_attn_paged.argtypes = [P(Cache), i32, vp, P(i64), vp, P(i64), f32, vp, vp, vp, i64, vp, sz, vp]
+    lib.sparsed_evict_workspace_bytes.argtypes = [P(Cache), P(sz)]
+    lib.sparsed_cache_evict.argtypes = [P(Cache), vp, i64, i32, i32, P(Cache), vp, i64, vp, vp, sz, vp]
     lib.sparsed_status_string.argtypes = [i32]
     lib.sparsed_status_string.restype = ctypes.c_char_p
     lib.sparsed_last_cuda_error.argtypes = []
@@ -383,3 +409,173 @@ def sparsed_last_device_status(ws: torch.Tensor) -> Tuple[int, int]:
     if st not in (0, 8):
         raise SparsedError(int(st), "sparsed_last_device_status")
     return code.value, where.value
+
+
+# ----------------------------------------------------------------------------- packed sequences and the paged cache
+_DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_FP16}
+_PACKED_RECORD = struct.Struct("@8i8qf%dx" % (ctypes.sizeof(Packed) - struct.calcsize("@8i8qf")))
+_TwoStrides = ctypes.c_int64 * 2
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
+    """The device of all of them, as its index (-1: not a CUDA device)."""
+    device = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != device:
+            raise ValueError("all tensors of a call must be on the same device")
+    return device
+
+
+def _call(device: int, what: str, function, *args) -> None:
+    """Calls a library function on the current stream of `device`, which the library finds as the current device."""
+    if device < 0:
+        raise ValueError(f"{what} needs CUDA tensors")
+    stream = torch._C._cuda_getCurrentRawStream(device)
+    if device == torch.cuda.current_device():
+        _check(function(*args, stream), what)
+    else:
+        with torch.cuda.device(device):
+            _check(function(*args, stream), what)
+
+
+def _row_strides(t: torch.Tensor, heads: Optional[int], what: str) -> Tuple[int, int]:
+    """Strides (row, head) of a [rows, heads, 128] tensor. (A dimension of one or no rows may have any stride.)"""
+    shape, strides = t.shape, t.stride()
+    _need(len(shape) == 3 and (heads is None or shape[1] == heads), f"{what} must be [rows, heads, head_dim]")
+    _need(strides[2] == 1, f"{what}: head_dim must be contiguous")
+    head = strides[1] if shape[1] > 1 else shape[2]
+    return (strides[0] if shape[0] > 1 else max(shape[1] * shape[2], head)), head
+
+
+def _int32(t: torch.Tensor, dims: int, what: str) -> None:
+    _need(t.dtype == torch.int32 and t.dim() == dims and (t.shape[-1] <= 1 or t.stride(-1) == 1),
+          f"{what} must be int32 with {dims} dimension(s), the last one contiguous")
+
+
+def _fp32(t: Optional[torch.Tensor], shape, what: str) -> Optional[int]:
+    if t is None:
+        return None
+    _need(t.dtype == torch.float32 and t.is_contiguous() and (shape is None or tuple(t.shape) == tuple(shape)),
+          f"{what} must be fp32 and contiguous" + (f", {tuple(shape)}" if shape is not None else ""))
+    return t.data_ptr()
+
+
+def sparsed_attn_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, cu_q: torch.Tensor,
+                        cu_k: torch.Tensor, ws: torch.Tensor, causal: bool = False, lse: Optional[torch.Tensor] = None,
+                        softmax_scale: float = 0.0) -> None:
+    """Attention over packed sequences: q, o [total_q, heads_q, 128], k, v [total_k, heads_kv, 128], bf16 or fp16;
+    sequence b owns rows cu_q[b]:cu_q[b+1] of q and o and cu_k[b]:cu_k[b+1] of k and v (int32). With `causal` a sequence's
+    queries are its last tokens. lse: fp32 [heads_q, total_q]. Rows behind the last sequence are left as they were."""
+    total_q, heads_q, head_dim = q.shape
+    total_k, heads_kv, _ = k.shape
+    device = _same_device(q, k, v, o, cu_q, cu_k, ws, lse)
+    _need(q.dtype in _DTYPES and q.dtype == k.dtype == v.dtype == o.dtype, "q, k, v, o must be all bf16 or all fp16")
+    _need(o.shape == q.shape and v.shape == k.shape and k.shape[2] == head_dim, "o must be shaped like q, v like k")
+    _int32(cu_q, 1, "cu_q")
+    _int32(cu_k, 1, "cu_k")
+    _need(cu_q.shape[0] == cu_k.shape[0] >= 1, "cu_q and cu_k must both be [num_seqs + 1]")
+    record = _PACKED_RECORD.pack(cu_q.shape[0] - 1, total_q, total_k, heads_q, heads_kv, head_dim, _DTYPES[q.dtype],
+                                 1 if causal else 0, *_row_strides(q, heads_q, "q"), *_row_strides(k, heads_kv, "k"),
+                                 *_row_strides(v, heads_kv, "v"), *_row_strides(o, heads_q, "o"), softmax_scale)
+    _call(device, "sparsed_attn_packed", load_library().sparsed_attn_packed, ctypes.byref(Packed.from_buffer_copy(record)),
+          cu_q.data_ptr(), cu_k.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+          _fp32(lse, (heads_q, total_q), "lse"), ws.data_ptr(), ws.numel())
+
+
+def make_cache(k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor) -> Cache:
+    """A paged key-value cache: pools k, v [num_pages, page_size, heads_kv, 128] (any strides with head_dim contiguous, so a
+    transposed view of [num_pages, heads_kv, page_size, 128] too), page_table int32 [batch, max_pages], seq_lens int32
+    [batch]. The calls read the tensors' contents when they run; make it once and keep it."""
+    _need(k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.dtype in _DTYPES,
+          "k and v must be [num_pages, page_size, heads_kv, head_dim], bf16 or fp16")
+    _need(k.stride(3) == 1 and v.stride(3) == 1, "head_dim must be contiguous")
+    _int32(page_table, 2, "page_table")
+    _int32(seq_lens, 1, "seq_lens")
+    _need(page_table.shape[0] == seq_lens.shape[0], "page_table and seq_lens must have the same batch")
+    _same_device(k, v, page_table, seq_lens)
+
+    def strides(t):   # a dimension of one place may have any stride
+        head = t.stride(2) if t.shape[2] > 1 else t.shape[3]
+        return (t.stride(0) if t.shape[0] > 1 else max(t.stride(1) * t.shape[1], head * t.shape[2])), t.stride(1), head
+
+    c = Cache(k.data_ptr(), v.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(),
+              page_table.stride(0) if page_table.shape[0] > 1 else 0, (ctypes.c_int64 * 3)(*strides(k)),
+              (ctypes.c_int64 * 3)(*strides(v)), k.shape[0], k.shape[1], k.shape[2], k.shape[3], page_table.shape[0],
+              page_table.shape[1], _DTYPES[k.dtype])
+    c.tensors = (k, v, page_table, seq_lens)
+    return c
+
+
+def sparsed_cache_write(cache: Cache, k_new: torch.Tensor, v_new: torch.Tensor, cu_new: torch.Tensor,
+                        ws: torch.Tensor) -> None:
+    """New tokens' keys and values [total_new, heads_kv, 128] to the last positions of their sequences (seq_lens counts them
+    already); sequence b's are rows cu_new[b]:cu_new[b+1]."""
+    pool = cache.tensors[0]
+    device = _same_device(pool, k_new, v_new, cu_new, ws)
+    _need(k_new.dtype == v_new.dtype == pool.dtype, "k_new and v_new must have the cache's type")
+    _need(k_new.shape == v_new.shape and k_new.dim() == 3 and k_new.shape[2] == cache.head_dim,
+          "k_new and v_new must be [total_new, heads_kv, head_dim]")
+    _int32(cu_new, 1, "cu_new")
+    _need(cu_new.shape[0] == cache.batch + 1, "cu_new must be [batch + 1]")
+    _call(device, "sparsed_cache_write", load_library().sparsed_cache_write, ctypes.byref(cache), k_new.data_ptr(),
+          _TwoStrides(*_row_strides(k_new, cache.heads_kv, "k_new")), v_new.data_ptr(),
+          _TwoStrides(*_row_strides(v_new, cache.heads_kv, "v_new")), cu_new.data_ptr(), k_new.shape[0], ws.data_ptr(),
+          ws.numel())
+
+
+def sparsed_paged_workspace_bytes(cache: Cache, heads_q: int, with_mass: bool = False) -> int:
+    out = ctypes.c_size_t()
+    _check(load_library().sparsed_paged_workspace_bytes(ctypes.byref(cache), int(heads_q), 1 if with_mass else 0,
+                                                        ctypes.byref(out)), "sparsed_paged_workspace_bytes")
+    return int(out.value)
+
+
+def sparsed_attn_paged(q: torch.Tensor, cache: Cache, o: torch.Tensor, ws: torch.Tensor,
+                       lse: Optional[torch.Tensor] = None, mass_in: Optional[torch.Tensor] = None,
+                       mass_out: Optional[torch.Tensor] = None, softmax_scale: float = 0.0) -> None:
+    """One new token per sequence, q, o [batch, heads_q, 128], over its cached keys. lse: fp32 [batch, heads_q].
+    mass_out: fp32 [batch, heads_kv, capacity], receives mass_in (the same tensor, another, or None: zeros) plus each cached
+    key's attention weight, summed over the query heads of its group."""
+    batch, heads_q, head_dim = q.shape
+    pool = cache.tensors[0]
+    device = _same_device(pool, q, o, ws, lse, mass_in, mass_out)
+    _need(q.dtype == o.dtype == pool.dtype, "q and o must have the cache's type")
+    _need(batch == cache.batch and head_dim == cache.head_dim and o.shape == q.shape, "q and o must be [batch, heads_q, head_dim]")
+    capacity, in_ptr, out_ptr = 0, None, None
+    if mass_out is not None or mass_in is not None:
+        _need(mass_out is not None, "mass_in needs mass_out")
+        _need(mass_out.dim() == 3, "mass_out must be [batch, heads_kv, capacity]")
+        capacity = mass_out.shape[2]
+        in_ptr = _fp32(mass_in, (batch, cache.heads_kv, capacity), "mass_in")
+        out_ptr = _fp32(mass_out, (batch, cache.heads_kv, capacity), "mass_out")
+    _call(device, "sparsed_attn_paged", load_library().sparsed_attn_paged, ctypes.byref(cache), heads_q, q.data_ptr(),
+          _TwoStrides(*_row_strides(q, heads_q, "q")), o.data_ptr(), _TwoStrides(*_row_strides(o, heads_q, "o")),
+          softmax_scale, _fp32(lse, (batch, heads_q), "lse"), in_ptr, out_ptr, capacity, ws.data_ptr(), ws.numel())
+
+
+def sparsed_evict_workspace_bytes(cache: Cache) -> int:
+    out = ctypes.c_size_t()
+    _check(load_library().sparsed_evict_workspace_bytes(ctypes.byref(cache), ctypes.byref(out)),
+           "sparsed_evict_workspace_bytes")
+    return int(out.value)
+
+
+def sparsed_cache_evict(cache: Cache, mass: torch.Tensor, keep: int, recent: int, to: Cache, mass_out: torch.Tensor,
+                        kept: torch.Tensor, ws: torch.Tensor) -> None:
+    """Moves, for every sequence and key-value head, the `recent` last keys and those with the largest mass, min(keep, length)
+    in all, in their order, to the pages of `to`, whose seq_lens are written. mass: fp32 [batch, heads_kv, capacity];
+    mass_out: fp32 [batch, heads_kv, new capacity]; kept: int32 [batch, heads_kv, keep], the kept positions, then -1."""
+    device = _same_device(cache.tensors[0], to.tensors[0], mass, mass_out, kept, ws)
+    _need(mass.dim() == 3 and mass_out.dim() == 3, "mass and mass_out must be [batch, heads_kv, capacity]")
+    rows = (cache.batch, cache.heads_kv)
+    _need(kept.dtype == torch.int32 and kept.is_contiguous() and tuple(kept.shape) == rows + (keep,),
+          "kept must be int32 and contiguous, [batch, heads_kv, keep]")
+    _call(device, "sparsed_cache_evict", load_library().sparsed_cache_evict, ctypes.byref(cache),
+          _fp32(mass, rows + (mass.shape[2],), "mass"), mass.shape[2], int(keep), int(recent), ctypes.byref(to),
+          _fp32(mass_out, rows + (mass_out.shape[2],), "mass_out"), mass_out.shape[2], kept.data_ptr(), ws.data_ptr(),
+          ws.numel())

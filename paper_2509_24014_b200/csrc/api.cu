@@ -9,6 +9,7 @@
 #include "../../include/sparsed.h"
 #include "dense_choice.h"
 #include "internal.h"
+#include "packed_and_paged.h"
 
 namespace {
 
@@ -302,6 +303,8 @@ sparsed_status sparsed_workspace_bytes(int32_t op, const sparsed_shape* shape, c
     case SPARSED_OP_ATTN_SPARSE:
     case SPARSED_OP_SELECT_FROM_SCORES:
     case SPARSED_OP_PATTERN_VALIDATE:
+    case SPARSED_OP_ATTN_PACKED:
+    case SPARSED_OP_CACHE_WRITE:
       *out_bytes = SPARSED_STATUS_BYTES;
       return SPARSED_OK;
     case SPARSED_OP_SELECT_PATTERN: {
@@ -793,6 +796,278 @@ sparsed_status sparsed_last_device_status(void* ws, void* cuda_stream, int32_t* 
 }
 
 }  // extern "C"
+
+// ------------------------------------------------------------------------------------------
+// Packed sequences and the paged key-value cache
+// ------------------------------------------------------------------------------------------
+namespace {
+
+// Strides of a [rows, heads, 128] tensor (row, head), all-zero = contiguous.
+sparsed_status row_strides(const int64_t in[2], int heads, int64_t out[2]) {
+  const bool given = in != nullptr && (in[0] != 0 || in[1] != 0);
+  out[0] = given ? in[0] : static_cast<int64_t>(heads) * 128;
+  out[1] = given ? in[1] : 128;
+  if (out[0] <= 0 || out[1] <= 0) return SPARSED_ERR_INVALID_ARG;
+  if (out[0] % 8 != 0 || out[1] % 8 != 0) return SPARSED_ERR_ALIGNMENT;
+  if (out[0] < 128 || out[1] < 128) return SPARSED_ERR_INVALID_ARG;
+  return SPARSED_OK;
+}
+
+sparsed_status check_scale(float scale, float* scale_log2) {
+  if (!(scale >= 0.f) || !std::isfinite(scale)) return SPARSED_ERR_INVALID_ARG;
+  *scale_log2 = (scale == 0.f ? 1.0f / std::sqrt(128.f) : scale) * 1.44269504088896341f;
+  return SPARSED_OK;
+}
+
+// The sizes of a cache alone (what the workspace queries need).
+sparsed_status check_cache_sizes(const sparsed_cache* c) {
+  if (c == nullptr) return SPARSED_ERR_INVALID_ARG;
+  if (c->num_pages < 1 || c->heads_kv < 1 || c->batch < 1 || c->max_pages < 1) return SPARSED_ERR_INVALID_ARG;
+  if (c->head_dim != 128) return SPARSED_ERR_UNSUPPORTED;
+  if (c->dtype != SPARSED_DTYPE_BF16 && c->dtype != SPARSED_DTYPE_FP16) return SPARSED_ERR_UNSUPPORTED;
+  if (c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1)) != 0) return SPARSED_ERR_UNSUPPORTED;
+  // positions of a sequence, and (sequence, head) pairs, are counted in 32 bits
+  if (static_cast<int64_t>(c->max_pages) * c->page_size > (INT32_MAX >> 1)) return SPARSED_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(c->batch) * c->heads_kv > (INT32_MAX >> 5)) return SPARSED_ERR_UNSUPPORTED;
+  return SPARSED_OK;
+}
+
+sparsed_status check_cache(const sparsed_cache* c, CacheView* view) {
+  sparsed_status st = check_cache_sizes(c);
+  if (st != SPARSED_OK) return st;
+  if (c->k == nullptr || c->v == nullptr || c->page_table == nullptr || c->seq_lens == nullptr) return SPARSED_ERR_INVALID_ARG;
+  if (!aligned16(c->k) || !aligned16(c->v) || !aligned4(c->page_table) || !aligned4(c->seq_lens)) return SPARSED_ERR_ALIGNMENT;
+  view->k = static_cast<uint16_t*>(c->k);
+  view->v = static_cast<uint16_t*>(c->v);
+  view->table = c->page_table;
+  view->lens = c->seq_lens;
+  view->table_stride = c->table_stride == 0 ? c->max_pages : c->table_stride;
+  if (view->table_stride < 0) return SPARSED_ERR_INVALID_ARG;
+  const int64_t* given[2] = {c->k_strides, c->v_strides};
+  int64_t* page[2] = {&view->k_page, &view->v_page};
+  int64_t* place[2] = {&view->k_place, &view->v_place};
+  int64_t* head[2] = {&view->k_head, &view->v_head};
+  for (int i = 0; i < 2; ++i) {
+    const int64_t* s = given[i];
+    const bool contiguous = s[0] == 0 && s[1] == 0 && s[2] == 0;
+    *head[i] = contiguous ? 128 : s[2];
+    *place[i] = contiguous ? 128ll * c->heads_kv : s[1];
+    *page[i] = contiguous ? 128ll * c->heads_kv * c->page_size : s[0];
+    const int64_t all[3] = {*page[i], *place[i], *head[i]};
+    for (int64_t x : all) {
+      if (x < 128) return SPARSED_ERR_INVALID_ARG;
+      if (x % 8 != 0) return SPARSED_ERR_ALIGNMENT;
+    }
+  }
+  view->num_pages = c->num_pages;
+  view->page_shift = 0;
+  while ((1 << view->page_shift) < c->page_size) ++view->page_shift;
+  view->heads_kv = c->heads_kv;
+  view->batch = c->batch;
+  view->max_pages = c->max_pages;
+  return SPARSED_OK;
+}
+
+}  // namespace
+
+extern "C" sparsed_status sparsed_attn_packed(const sparsed_packed* shape, const int32_t* cu_q, const int32_t* cu_k,
+                                              const void* q, const void* k, const void* v, void* o, float* lse_or_null,
+                                              void* ws, size_t ws_bytes, void* cuda_stream) {
+  if (shape == nullptr) return SPARSED_ERR_INVALID_ARG;
+  if (shape->num_seqs < 0 || shape->total_q < 0 || shape->total_k < 0 || shape->heads_q < 1 || shape->heads_kv < 1)
+    return SPARSED_ERR_INVALID_ARG;
+  if (shape->heads_q % shape->heads_kv != 0) return SPARSED_ERR_INVALID_ARG;
+  if (shape->causal != 0 && shape->causal != 1) return SPARSED_ERR_INVALID_ARG;
+  if (shape->head_dim != 128) return SPARSED_ERR_UNSUPPORTED;
+  if (shape->dtype != SPARSED_DTYPE_BF16 && shape->dtype != SPARSED_DTYPE_FP16) return SPARSED_ERR_UNSUPPORTED;
+  PackedParams p;
+  int64_t qs[2], ks[2], vs[2], os[2];
+  sparsed_status st;
+  if ((st = check_scale(shape->softmax_scale, &p.scale_log2)) != SPARSED_OK) return st;
+  if ((st = row_strides(shape->q_strides, shape->heads_q, qs)) != SPARSED_OK) return st;
+  if ((st = row_strides(shape->k_strides, shape->heads_kv, ks)) != SPARSED_OK) return st;
+  if ((st = row_strides(shape->v_strides, shape->heads_kv, vs)) != SPARSED_OK) return st;
+  if ((st = row_strides(shape->o_strides, shape->heads_q, os)) != SPARSED_OK) return st;
+  const int64_t tiles = static_cast<int64_t>(shape->total_q) / 128 + shape->num_seqs;
+  if (tiles * shape->heads_q > INT32_MAX) return SPARSED_ERR_UNSUPPORTED;
+  const bool nothing = shape->num_seqs == 0 || shape->total_q == 0, no_keys = shape->total_k == 0;
+  if (cu_q == nullptr || cu_k == nullptr) return SPARSED_ERR_INVALID_ARG;
+  if (!nothing && (q == nullptr || o == nullptr)) return SPARSED_ERR_INVALID_ARG;
+  if (!nothing && !no_keys && (k == nullptr || v == nullptr)) return SPARSED_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned4(cu_q) || !aligned4(cu_k) ||
+      !aligned4(lse_or_null))
+    return SPARSED_ERR_ALIGNMENT;
+  if ((st = check_ws(ws, ws_bytes, SPARSED_STATUS_BYTES)) != SPARSED_OK) return st;
+  if (nothing) return SPARSED_OK;
+  if ((st = check_arch()) != SPARSED_OK) return st;
+  CUtensorMap tq, tk, tv;
+  const int64_t q3[3] = {qs[0], qs[1], qs[0]}, k3[3] = {ks[0], ks[1], ks[0]}, v3[3] = {vs[0], vs[1], vs[0]};
+  if ((st = make_tensor_map(&tq, q, 1, shape->heads_q, shape->total_q, q3, 128)) != SPARSED_OK) return st;
+  if (no_keys) {
+    tk = tv = tq;   // (nothing is loaded through them)
+  } else {
+    if ((st = make_tensor_map(&tk, k, 1, shape->heads_kv, shape->total_k, k3, 64)) != SPARSED_OK) return st;
+    if ((st = make_tensor_map(&tv, v, 1, shape->heads_kv, shape->total_k, v3, 64)) != SPARSED_OK) return st;
+  }
+  p.cu_q = cu_q;
+  p.cu_k = cu_k;
+  p.o = o;
+  p.o_stride_t = os[0];
+  p.o_stride_h = os[1];
+  p.v = v;
+  p.v_stride_t = vs[0];
+  p.v_stride_h = vs[1];
+  p.lse = lse_or_null;
+  p.num_seqs = shape->num_seqs;
+  p.total_q = shape->total_q;
+  p.total_k = shape->total_k;
+  p.heads_q = shape->heads_q;
+  p.group = shape->heads_q / shape->heads_kv;
+  p.causal = shape->causal;
+  p.tiles = static_cast<int>(tiles);
+  // key-value heads whose K and V (512 bytes a key) take 48 MB of the L2 together, one at least
+  const int64_t heads_in_l2 = (int64_t{48} << 20) / (512ll * (shape->total_k > 0 ? shape->total_k : 1));
+  p.heads_per_pass = static_cast<int>(heads_in_l2 >= shape->heads_kv ? shape->heads_q
+                                                                     : (heads_in_l2 > 1 ? heads_in_l2 : 1) * p.group);
+  p.max_ctas = attn_max_ctas();
+  p.slow_path_events = reinterpret_cast<unsigned long long*>(static_cast<uint8_t*>(ws) + 32);
+  p.status = static_cast<DeviceStatus*>(ws);
+  cudaError_t e = launch_attn_packed(tq, tk, tv, p, shape->dtype == SPARSED_DTYPE_FP16, static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? SPARSED_OK : cuda_fail(e);
+}
+
+extern "C" sparsed_status sparsed_cache_write(const sparsed_cache* cache, const void* k_new, const int64_t k_new_strides[2],
+                                              const void* v_new, const int64_t v_new_strides[2], const int32_t* cu_new,
+                                              int32_t total_new, void* ws, size_t ws_bytes, void* cuda_stream) {
+  CacheWriteParams p;
+  sparsed_status st = check_cache(cache, &p.cache);
+  if (st != SPARSED_OK) return st;
+  if (total_new < 0 || cu_new == nullptr) return SPARSED_ERR_INVALID_ARG;
+  int64_t ks[2], vs[2];
+  if ((st = row_strides(k_new_strides, cache->heads_kv, ks)) != SPARSED_OK) return st;
+  if ((st = row_strides(v_new_strides, cache->heads_kv, vs)) != SPARSED_OK) return st;
+  if (total_new > 0 && (k_new == nullptr || v_new == nullptr)) return SPARSED_ERR_INVALID_ARG;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned4(cu_new)) return SPARSED_ERR_ALIGNMENT;
+  if ((st = check_ws(ws, ws_bytes, SPARSED_STATUS_BYTES)) != SPARSED_OK) return st;
+  if (total_new == 0) return SPARSED_OK;
+  if ((st = check_arch()) != SPARSED_OK) return st;
+  p.k = static_cast<const uint16_t*>(k_new);
+  p.v = static_cast<const uint16_t*>(v_new);
+  p.k_token = ks[0];
+  p.k_head = ks[1];
+  p.v_token = vs[0];
+  p.v_head = vs[1];
+  p.cu = cu_new;
+  p.total = total_new;
+  p.status = static_cast<DeviceStatus*>(ws);
+  cudaError_t e = launch_cache_write(p, static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? SPARSED_OK : cuda_fail(e);
+}
+
+// The sizes of a paged call: query heads, and units of work that are counted in 32 bits.
+static sparsed_status check_paged_sizes(const sparsed_cache* cache, int32_t heads_q) {
+  sparsed_status st = check_cache_sizes(cache);
+  if (st != SPARSED_OK) return st;
+  if (heads_q < 1 || heads_q % cache->heads_kv != 0) return SPARSED_ERR_INVALID_ARG;
+  const int64_t keys = static_cast<int64_t>(cache->max_pages) * cache->page_size;
+  if (static_cast<int64_t>(cache->batch) * heads_q * (keys / 64 + 1) > INT32_MAX) return SPARSED_ERR_UNSUPPORTED;
+  return SPARSED_OK;
+}
+
+extern "C" sparsed_status sparsed_paged_workspace_bytes(const sparsed_cache* cache, int32_t heads_q, int32_t with_mass,
+                                                        size_t* out_bytes) {
+  if (out_bytes == nullptr) return SPARSED_ERR_INVALID_ARG;
+  sparsed_status st = check_paged_sizes(cache, heads_q);
+  if (st != SPARSED_OK) return st;
+  *out_bytes = static_cast<size_t>(paged_layout(cache->batch, cache->heads_kv, heads_q / cache->heads_kv, cache->max_pages,
+                                                cache->page_size, with_mass != 0).bytes);
+  return SPARSED_OK;
+}
+
+extern "C" sparsed_status sparsed_attn_paged(const sparsed_cache* cache, int32_t heads_q, const void* q,
+                                             const int64_t q_strides[2], void* o, const int64_t o_strides[2],
+                                             float softmax_scale, float* lse_or_null, const float* mass_in_or_null,
+                                             float* mass_out_or_null, int64_t mass_capacity, void* ws, size_t ws_bytes,
+                                             void* cuda_stream) {
+  PagedParams p;
+  sparsed_status st = check_paged_sizes(cache, heads_q);
+  if (st != SPARSED_OK) return st;
+  if ((st = check_cache(cache, &p.cache)) != SPARSED_OK) return st;
+  if ((st = check_scale(softmax_scale, &p.scale_log2)) != SPARSED_OK) return st;
+  int64_t qs[2], os[2];
+  if ((st = row_strides(q_strides, heads_q, qs)) != SPARSED_OK) return st;
+  if ((st = row_strides(o_strides, heads_q, os)) != SPARSED_OK) return st;
+  if (q == nullptr || o == nullptr) return SPARSED_ERR_INVALID_ARG;
+  const bool with_mass = mass_out_or_null != nullptr;
+  if (!with_mass && mass_in_or_null != nullptr) return SPARSED_ERR_INVALID_ARG;
+  if (with_mass && mass_capacity < static_cast<int64_t>(cache->max_pages) * cache->page_size) return SPARSED_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(o) || !aligned4(lse_or_null) || !aligned4(mass_in_or_null) || !aligned4(mass_out_or_null))
+    return SPARSED_ERR_ALIGNMENT;
+  const int group = heads_q / cache->heads_kv;
+  const PagedLayout at = paged_layout(cache->batch, cache->heads_kv, group, cache->max_pages, cache->page_size, with_mass);
+  if ((st = check_ws(ws, ws_bytes, static_cast<size_t>(at.bytes))) != SPARSED_OK) return st;
+  if ((st = check_arch()) != SPARSED_OK) return st;
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  p.q = static_cast<const uint16_t*>(q);
+  p.o = static_cast<uint16_t*>(o);
+  p.q_seq = qs[0];
+  p.q_head = qs[1];
+  p.o_seq = os[0];
+  p.o_head = os[1];
+  p.lse = lse_or_null;
+  p.mass_in = mass_in_or_null;
+  p.mass_out = mass_out_or_null;
+  p.mass_capacity = mass_capacity;
+  p.group = group;
+  p.ctas = 0;
+  p.prefix = reinterpret_cast<int32_t*>(base + at.prefix);
+  p.lse2 = reinterpret_cast<float*>(base + at.lse2);
+  p.part_ml = reinterpret_cast<float2*>(base + at.part_ml);
+  p.part_o = reinterpret_cast<float*>(base + at.part_o);
+  p.logits = with_mass ? reinterpret_cast<float*>(base + at.logits) : nullptr;
+  p.status = static_cast<DeviceStatus*>(ws);
+  cudaError_t e = launch_attn_paged(p, attn_max_ctas() / 2, cache->dtype == SPARSED_DTYPE_FP16, static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? SPARSED_OK : cuda_fail(e);
+}
+
+extern "C" sparsed_status sparsed_evict_workspace_bytes(const sparsed_cache* from, size_t* out_bytes) {
+  if (out_bytes == nullptr) return SPARSED_ERR_INVALID_ARG;
+  sparsed_status st = check_cache_sizes(from);
+  if (st != SPARSED_OK) return st;
+  *out_bytes = SPARSED_STATUS_BYTES;
+  return SPARSED_OK;
+}
+
+extern "C" sparsed_status sparsed_cache_evict(const sparsed_cache* from, const float* mass, int64_t mass_capacity, int32_t keep,
+                                              int32_t recent, const sparsed_cache* to, float* mass_out,
+                                              int64_t mass_out_capacity, int32_t* kept, void* ws, size_t ws_bytes,
+                                              void* cuda_stream) {
+  EvictParams p;
+  sparsed_status st = check_cache(from, &p.from);
+  if (st != SPARSED_OK) return st;
+  if ((st = check_cache(to, &p.to)) != SPARSED_OK) return st;
+  if (from->batch != to->batch || from->heads_kv != to->heads_kv || from->dtype != to->dtype) return SPARSED_ERR_INVALID_ARG;
+  if (from->seq_lens == to->seq_lens) return SPARSED_ERR_INVALID_ARG;
+  if (mass == nullptr || mass_out == nullptr || kept == nullptr || mass == mass_out) return SPARSED_ERR_INVALID_ARG;
+  if (keep < 1 || recent < 0 || recent > keep) return SPARSED_ERR_INVALID_ARG;
+  if (keep > static_cast<int64_t>(to->max_pages) * to->page_size) return SPARSED_ERR_INVALID_ARG;
+  if (mass_capacity < static_cast<int64_t>(from->max_pages) * from->page_size || mass_out_capacity < keep)
+    return SPARSED_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(from->batch) * from->heads_kv * (keep / 64 + 1ll) > INT32_MAX) return SPARSED_ERR_UNSUPPORTED;
+  if (!aligned4(mass) || !aligned4(mass_out) || !aligned4(kept)) return SPARSED_ERR_ALIGNMENT;
+  if ((st = check_ws(ws, ws_bytes, SPARSED_STATUS_BYTES)) != SPARSED_OK) return st;
+  if ((st = check_arch()) != SPARSED_OK) return st;
+  p.mass = mass;
+  p.mass_out = mass_out;
+  p.mass_capacity = mass_capacity;
+  p.mass_out_capacity = mass_out_capacity;
+  p.kept = kept;
+  p.keep = keep;
+  p.recent = recent;
+  p.status = static_cast<DeviceStatus*>(ws);
+  cudaError_t e = launch_cache_evict(p, static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? SPARSED_OK : cuda_fail(e);
+}
 
 // ------------------------------------------------------------------------------------------
 // Selection without a caller workspace: the scratch lives in this library's device image.

@@ -11,9 +11,40 @@
 // far rescaled by 2^(m_old - m_new).
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include "sm100_primitives.cuh"
 
 namespace sparsed {
+
+// The 16-bit type of Q, K, V, P and O. (Most calls take bf16 only; the packed ones fp16 too.)
+struct Bf16Type {
+  static constexpr uint32_t kExponents = 0x7f807f80u;     // exponent bits of a pair
+  static constexpr uint32_t kExponentCarry = 0x00800080u; // added to them: bit 15 / 31 is set where all were ones
+  static __host__ __device__ constexpr uint32_t idesc(uint32_t bf16) { return bf16; }
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack_bf16x2(lo, hi); }
+  static __device__ __forceinline__ float2 unpack(uint32_t x) {
+    return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+  }
+};
+struct Fp16Type {
+  static constexpr uint32_t kExponents = 0x7c007c00u;
+  static constexpr uint32_t kExponentCarry = 0x04000400u;
+  static __host__ __device__ constexpr uint32_t idesc(uint32_t bf16) { return bf16 & ~((1u << 7) | (1u << 10)); }   // both formats 0: fp16
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t x) {
+    return __half22float2(*reinterpret_cast<const __half2*>(&x));
+  }
+};
+// Non-zero where one of the pair's two numbers is an infinity or NaN.
+template <class Type>
+__device__ __forceinline__ uint32_t non_finite_pair(uint32_t x) {
+  return ((x & Type::kExponents) + Type::kExponentCarry) & 0x80008000u;
+}
 
 // Running softmax state of one query row.
 struct RowState {
@@ -34,6 +65,7 @@ __device__ __forceinline__ void mask_columns_from(uint32_t (&r0)[32], uint32_t (
 // 2j, 2j+1) and returns the sums of p over columns 0-31 and 32-63. Every exponential is one
 // ex2.approx (moving a quarter or a half of them to an FMA-pipe polynomial was measured and lost
 // 4 % and 10 %: the softmax warps are bound by instruction issue and latency, not by the SFU).
+template <class Type = Bf16Type>
 __device__ __forceinline__ float2 softmax_group_fast(const uint32_t (&r0)[32], const uint32_t (&r1)[32],
                                                      float scale_log2, float m, uint32_t (&pk)[32]) {
   const float2 sc = make_float2(scale_log2, scale_log2);
@@ -47,8 +79,8 @@ __device__ __forceinline__ float2 softmax_group_fast(const uint32_t (&r0)[32], c
     const float2 e1 = make_float2(fast_exp2(x1.x), fast_exp2(x1.y));
     acc0 = __fadd2_rn(acc0, e0);
     acc1 = __fadd2_rn(acc1, e1);
-    pk[j] = pack_bf16x2(e0.x, e0.y);
-    pk[16 + j] = pack_bf16x2(e1.x, e1.y);
+    pk[j] = Type::pack(e0.x, e0.y);
+    pk[16 + j] = Type::pack(e1.x, e1.y);
   }
   return make_float2(acc0.x + acc0.y, acc1.x + acc1.y);
 }
@@ -289,6 +321,7 @@ __device__ __forceinline__ void store_output_row(uint32_t t_acc_row, bool have_a
 // O / l -> bf16, 64 columns of this thread's row, from tensor memory into a shared-memory tile of 128 rows x 64 columns of
 // bf16 (128 bytes a row; 1024-byte aligned), 128-byte swizzle as the tensor maps use it: the 16-byte chunk c of row r sits
 // at chunk c ^ (r & 7). t_acc: the columns' tensor-memory address in this row; have_acc = false writes zeros.
+template <class Type = Bf16Type>
 __device__ __forceinline__ void stage_output_half(uint32_t t_acc, bool have_acc, float inv_l, __nv_bfloat16* half_tile,
                                                   int row) {
   uint8_t* base = reinterpret_cast<uint8_t*>(half_tile) + row * 128;
@@ -306,13 +339,13 @@ __device__ __forceinline__ void stage_output_half(uint32_t t_acc, bool have_acc,
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       uint4 out;
-      out.x = pack_bf16x2(mul_keep_denormals(__uint_as_float(r[8 * g + 0]), inv_l),
+      out.x = Type::pack(mul_keep_denormals(__uint_as_float(r[8 * g + 0]), inv_l),
                           mul_keep_denormals(__uint_as_float(r[8 * g + 1]), inv_l));
-      out.y = pack_bf16x2(mul_keep_denormals(__uint_as_float(r[8 * g + 2]), inv_l),
+      out.y = Type::pack(mul_keep_denormals(__uint_as_float(r[8 * g + 2]), inv_l),
                           mul_keep_denormals(__uint_as_float(r[8 * g + 3]), inv_l));
-      out.z = pack_bf16x2(mul_keep_denormals(__uint_as_float(r[8 * g + 4]), inv_l),
+      out.z = Type::pack(mul_keep_denormals(__uint_as_float(r[8 * g + 4]), inv_l),
                           mul_keep_denormals(__uint_as_float(r[8 * g + 5]), inv_l));
-      out.w = pack_bf16x2(mul_keep_denormals(__uint_as_float(r[8 * g + 6]), inv_l),
+      out.w = Type::pack(mul_keep_denormals(__uint_as_float(r[8 * g + 6]), inv_l),
                           mul_keep_denormals(__uint_as_float(r[8 * g + 7]), inv_l));
       *reinterpret_cast<uint4*>(base + (((4 * c + g) ^ sw) << 4)) = out;
     }
@@ -347,15 +380,16 @@ struct UmmaTile64 {
 };
 
 // S[tmem_s] = Q K^T: eight M128 N64 K16 MMAs. q_lo / k_lo: low descriptor words of the two operands.
+template <class Type = Bf16Type>
 __device__ __forceinline__ void issue_qk64(uint32_t tmem_s, uint32_t q_lo, uint32_t k_lo, uint64_t* done) {
   tc_fence_after();
   if (elect_one_sync()) {
-    umma_ss_words<false>(tmem_s, q_lo, UmmaTile64::kHi, k_lo, UmmaTile64::kHi, UmmaTile64::kIdescQK);
+    umma_ss_words<false>(tmem_s, q_lo, UmmaTile64::kHi, k_lo, UmmaTile64::kHi, Type::idesc(UmmaTile64::kIdescQK));
 #pragma unroll
     for (int kk = 1; kk < 8; ++kk) {
       umma_ss_words<true>(tmem_s, q_lo + (kk >> 2) * UmmaTile64::kQHalfStep + (kk & 3) * 2, UmmaTile64::kHi,
                           k_lo + (kk >> 2) * UmmaTile64::kHalfStep + (kk & 3) * 2, UmmaTile64::kHi,
-                          UmmaTile64::kIdescQK);
+                          Type::idesc(UmmaTile64::kIdescQK));
     }
     umma_commit(done);
   }
@@ -378,14 +412,15 @@ __device__ __forceinline__ void issue_qk64_ts(uint32_t tmem_s, uint32_t tmem_q, 
 
 // O[tmem_o] (+)= P[tmem_p] V: four M128 N128 K16 MMAs with P (bf16 pairs) read from tensor memory.
 // v_lo: low descriptor word of the V tile as an MN-major operand (16 keys are 2048 bytes apart).
+template <class Type = Bf16Type>
 __device__ __forceinline__ void issue_pv64(uint32_t tmem_o, uint32_t tmem_p, uint32_t v_lo, bool accumulate,
                                            uint64_t* done) {
   tc_fence_after();
   if (elect_one_sync()) {
-    umma_ts_words(tmem_o, tmem_p, v_lo, UmmaTile64::kHi, UmmaTile64::kIdescPV, accumulate ? 1u : 0u);
+    umma_ts_words(tmem_o, tmem_p, v_lo, UmmaTile64::kHi, Type::idesc(UmmaTile64::kIdescPV), accumulate ? 1u : 0u);
 #pragma unroll
     for (int kk = 1; kk < 4; ++kk)
-      umma_ts_words(tmem_o, tmem_p + kk * 8, v_lo + kk * 128, UmmaTile64::kHi, UmmaTile64::kIdescPV, 1u);
+      umma_ts_words(tmem_o, tmem_p + kk * 8, v_lo + kk * 128, UmmaTile64::kHi, Type::idesc(UmmaTile64::kIdescPV), 1u);
     umma_commit(done);
   }
   __syncwarp();
