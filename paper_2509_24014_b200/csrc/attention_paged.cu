@@ -60,11 +60,13 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   return y;
 }
 
-// 16 bytes into four words, or zeros; each byte of the cache is read by one warp only, so it need not stay in L1.
-__device__ __forceinline__ void load_once(uint32_t* x, const uint16_t* p, bool wanted) {
+// 16 bytes into four words. (Each byte of the cache is read by one warp only, so it need not stay in L1.)
+__device__ __forceinline__ void load_once(uint32_t* x, const uint16_t* p) {
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "l"(p));
+}
+__device__ __forceinline__ void load_once_if(uint32_t* x, const uint16_t* p, bool wanted) {
   x[0] = x[1] = x[2] = x[3] = 0u;
-  if (wanted)
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "l"(p));
+  if (wanted) load_once(x, p);
 }
 
 __device__ __forceinline__ int units_of(int len) { return (len + kUnit - 1) / kUnit; }
@@ -80,7 +82,7 @@ struct PagedSmem {
   int found_seq, found_units;
 };
 
-template <class Type, int kHeads>
+template <class Type, int kHeads, bool kMass>
 __global__ void __launch_bounds__(kThreads, kHeads == 8 ? 4 : 3) attn_paged_kernel(const PagedParams p) {
   constexpr int kNT = kHeads / 8;
   __shared__ PagedSmem<kHeads> sm;
@@ -145,6 +147,7 @@ __global__ void __launch_bounds__(kThreads, kHeads == 8 ? 4 : 3) attn_paged_kern
 
   const float scale_log2 = p.scale_log2;
   const int place_mask = (1 << c.page_shift) - 1;
+  const int64_t room = static_cast<int64_t>(c.max_pages) << c.page_shift;   // logits per query head
 
   for (int unit = unit0; unit < unit1;) {
     // ---- a segment: units of one sequence and row -------------------------------------------
@@ -187,71 +190,93 @@ __global__ void __launch_bounds__(kThreads, kHeads == 8 ? 4 : 3) attn_paged_kern
       const int key0 = tile * kUnit + warp * kWarpKeys;
       return tile < tile1 && key0 < len ? page_of(c, seq, key0 >> c.page_shift, p.status, 12) : -1;
     };
-    // positions at and beyond `valid` are not read: zeros
+    const uint16_t* k_lane = c.k + kv_head * c.k_head + g * c.k_place + t * 8;
+    const uint16_t* v_lane = c.v + kv_head * c.v_head + 2 * t * c.v_place + g * 8;
+    // K and V of the warp's keys in a unit; positions at and beyond `valid` are not read: zeros
     auto load_k = [&](int page, int key0, int valid) {
-      const uint16_t* k = c.k + page * c.k_page + kv_head * c.k_head + ((key0 & place_mask) + g) * c.k_place + t * 8;
+      const uint16_t* k = k_lane + page * c.k_page + (key0 & place_mask) * c.k_place;
+      if (valid >= kWarpKeys) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r)
+        for (int r = 0; r < 2; ++r, k += 8 * c.k_place)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          load_once(kx[r] + 4 * i, k + r * 8 * c.k_place + i * 32, g + 8 * r < valid);
+          for (int i = 0; i < 4; ++i) load_once(kx[r] + 4 * i, k + i * 32);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 2; ++r, k += 8 * c.k_place)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) load_once_if(kx[r] + 4 * i, k + i * 32, g + 8 * r < valid);
+      }
     };
     auto load_v = [&](int page, int key0, int valid) {
-      const uint16_t* v = c.v + page * c.v_page + kv_head * c.v_head + (key0 & place_mask) * c.v_place + g * 8;
+      const uint16_t* v = v_lane + page * c.v_page + (key0 & place_mask) * c.v_place;
+      if (valid >= kWarpKeys) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int key = 2 * t + (r & 1) + 8 * (r >> 1);
+        for (int r = 0; r < 4; ++r, v += (r == 2 ? 7 : 1) * c.v_place) {   // keys 2t, 2t + 1, 2t + 8, 2t + 9
+          load_once(vx[r], v);
+          load_once(vx[r] + 4, v + 64);
+        }
+      } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          load_once(vx[r] + 4 * i, v + key * c.v_place + i * 64, key < valid);
+        for (int r = 0; r < 4; ++r, v += (r == 2 ? 7 : 1) * c.v_place) {
+          const bool wanted = 2 * t + (r & 1) + 8 * (r >> 1) < valid;
+          load_once_if(vx[r], v, wanted);
+          load_once_if(vx[r] + 4, v + 64, wanted);
+        }
       }
     };
     // valid keys of this warp in a unit: none where there is no page
-    auto valid_at = [&](int tile, int page) -> int { return page < 0 ? 0 : min(kWarpKeys, len - tile * kUnit - warp * kWarpKeys); };
+    auto valid_at = [&](int tile, int page) -> int { return page < 0 ? 0 : len - tile * kUnit - warp * kWarpKeys; };
 
     int page = page_at(tile0);
     int valid = valid_at(tile0, page);
     load_k(page, tile0 * kUnit + warp * kWarpKeys, valid);
     load_v(page, tile0 * kUnit + warp * kWarpKeys, valid);
     int next_page = page_at(tile0 + 1);
+    [[maybe_unused]] float* logits = nullptr;   // of key 0 + g, head 2t
+    if constexpr (kMass)
+      logits = p.logits + (static_cast<int64_t>(seq) * c.heads_kv * p.group + head0 + 2 * t) * room + g;
     __syncthreads();   // Q is there
     for (int tile = tile0; tile < tile1; ++tile) {
       const int key0 = tile * kUnit + warp * kWarpKeys;
       const int next_valid = valid_at(tile + 1, next_page);
-      // ---- S^T = K Q^T
+      // ---- S^T = K Q^T, in two chains of dependent instructions
       float s[kNT][4];
 #pragma unroll
       for (int n = 0; n < kNT; ++n) {
+        float s2[4] = {0.f, 0.f, 0.f, 0.f};
         s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const uint4 q = *reinterpret_cast<const uint4*>(&sm.q[n * 8 + g][(4 * i + t) * 8]);
           mma16816<Type>(s[n], kx[0][4 * i], kx[1][4 * i], kx[0][4 * i + 1], kx[1][4 * i + 1], q.x, q.y);
-          mma16816<Type>(s[n], kx[0][4 * i + 2], kx[1][4 * i + 2], kx[0][4 * i + 3], kx[1][4 * i + 3], q.z, q.w);
+          mma16816<Type>(s2, kx[0][4 * i + 2], kx[1][4 * i + 2], kx[0][4 * i + 3], kx[1][4 * i + 3], q.z, q.w);
         }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) s[n][x] = (s[n][x] + s2[x]) * scale_log2;
       }
       if (tile + 1 < tile1) load_k(next_page, key0 + kUnit, next_valid);
       const int page_after = page_at(tile + 2);
       // ---- probabilities
       if (valid > 0) {   // (the same for the whole warp)
+        if (valid < kWarpKeys) {
+#pragma unroll
+          for (int n = 0; n < kNT; ++n)
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              if (g + 8 * (x >> 1) >= valid) s[n][x] = -INFINITY;
+        }
         bool outgrown = false;
 #pragma unroll
         for (int n = 0; n < kNT; ++n)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            s[n][x] = g + 8 * (x >> 1) < valid ? s[n][x] * scale_log2 : -INFINITY;
-            outgrown = outgrown || s[n][x] > m[n][x & 1] + kSlack;
-          }
-        if (p.logits != nullptr) {
-          float* to = p.logits + ((static_cast<int64_t>(seq) * c.heads_kv + kv_head) * (static_cast<int64_t>(c.max_pages) << c.page_shift) + key0 + g) * p.group +
-                      (head0 - kv_head * p.group);
+          for (int x = 0; x < 2; ++x) outgrown = outgrown || fmaxf(s[n][x], s[n][x + 2]) > m[n][x] + kSlack;
+        if constexpr (kMass) {
 #pragma unroll
           for (int n = 0; n < kNT; ++n)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const int h = 8 * n + 2 * t + (x & 1);
-              if (h < heads && g + 8 * (x >> 1) < valid) to[static_cast<int64_t>(8 * (x >> 1)) * p.group + h] = s[n][x];
-            }
+            for (int x = 0; x < 4; ++x)
+              if (8 * n + 2 * t + (x & 1) < heads && g + 8 * (x >> 1) < valid)
+                logits[(8 * n + (x & 1)) * room + key0 + 8 * (x >> 1)] = s[n][x];
         }
         if (__any_sync(0xffffffffu, outgrown)) {
           // logits well above their head's reference (or there is none yet): the tile's maximum becomes the reference
@@ -461,12 +486,13 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p,
   }
   __syncthreads();
   const int64_t row = static_cast<int64_t>(seq) * c.heads_kv + kv_head;
-  const float* logits = p.logits + row * (static_cast<int64_t>(c.max_pages) << c.page_shift) * p.group;
+  const int64_t room = static_cast<int64_t>(c.max_pages) << c.page_shift;
+  const float* logits = p.logits + row * p.group * room;
   for (int j = key0 + tid; j < min(key0 + kMassKeys, len); j += kJoinThreads) {
     float sum = 0.f;
     const int page = page_of(c, seq, j >> c.page_shift, p.status, 12);   // (a key whose page is missing has no weight)
     if (page >= 0)
-      for (int h = 0; h < p.group; ++h) sum += fast_exp2(__ldcg(logits + static_cast<int64_t>(j) * p.group + h) - lse_of[h]);
+      for (int h = 0; h < p.group; ++h) sum += fast_exp2(__ldcg(logits + h * room + j) - lse_of[h]);
     const float had = p.mass_in != nullptr ? __ldcg(p.mass_in + row * p.mass_capacity + j) : 0.f;
     p.mass_out[row * p.mass_capacity + j] = had + sum;
   }
@@ -474,7 +500,9 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p,
 
 template <class Type, int kHeads>
 cudaError_t launch(const PagedParams& p, cudaStream_t stream) {
-  cudaError_t e = launch_overlapped(attn_paged_kernel<Type, kHeads>, p.ctas, p.ctas, kThreads, 0, stream, p);
+  cudaError_t e = p.mass_out != nullptr
+                      ? launch_overlapped(attn_paged_kernel<Type, kHeads, true>, p.ctas, p.ctas, kThreads, 0, stream, p)
+                      : launch_overlapped(attn_paged_kernel<Type, kHeads, false>, p.ctas, p.ctas, kThreads, 0, stream, p);
   if (e != cudaSuccess) return e;
   const int room = p.cache.max_pages << p.cache.page_shift;
   const int mass_blocks = p.mass_out != nullptr ? (room + kMassKeys - 1) / kMassKeys : 0;

@@ -66,7 +66,7 @@ struct PagedParams {
   float* lse2;             // [batch, heads_q] base-2 LSE of sequences that one CTA has done by itself
   float2* part_ml;         // [2 * ctas, heads per chunk] (reference, sum) of a part
   float* part_o;           // [2 * ctas, heads per chunk, 128]
-  float* logits;           // [batch, heads_kv, max_len, group] scaled base-2 logits, with mass_out only
+  float* logits;           // [batch, heads_q, max_pages * page_size] scaled base-2 logits, with mass_out only
   DeviceStatus* status;
 };
 struct PagedLayout {
