@@ -100,6 +100,37 @@ sparsed_status make_tensor_map(CUtensorMap* out, const void* base, int batch, in
   return SPARSED_OK;
 }
 
+// One pool of a paged cache: 16-bit [pages, places, heads, 128] with element strides (page, place, head) as [pages, heads, 2
+// halves, places, 64]; box = 64 x 16 places x both halves, 128B swizzle. Cached like the other maps (the sizes that tell two
+// maps apart go into the same key; box_rows = -1 keeps it from meeting theirs).
+sparsed_status make_pool_map(CUtensorMap* out, const void* base, int pages, int places, int heads, int64_t page_stride,
+                             int64_t place_stride, int64_t head_stride) {
+  TensorMapKey key{base, {page_stride, place_stride, head_stride}, pages, heads, places, -1};
+  TensorMapSlot& slot = g_tensor_maps[tensor_map_slot(key)];
+  if (slot.valid && slot.key == key) {
+    *out = slot.map;
+    return SPARSED_OK;
+  }
+  EncodeTiledFn enc = encode_tiled_fn();
+  if (enc == nullptr) return cuda_fail(cudaErrorNotSupported);
+  cuuint64_t dims[5] = {64, static_cast<cuuint64_t>(places), 2, static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(pages)};
+  cuuint64_t gstrides[4] = {static_cast<cuuint64_t>(place_stride) * 2, 128, static_cast<cuuint64_t>(head_stride) * 2,
+                            static_cast<cuuint64_t>(page_stride) * 2};
+  cuuint32_t box[5] = {64, 16, 2, 1, 1};
+  cuuint32_t elem[5] = {1, 1, 1, 1, 1};
+  CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, gstrides, box, elem,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    g_last_cuda_error = static_cast<int32_t>(r);
+    return SPARSED_ERR_CUDA;
+  }
+  slot.key = key;
+  slot.map = *out;
+  slot.valid = true;
+  return SPARSED_OK;
+}
+
 struct Resolved {
   int64_t q[3], k[3], v[3], o[3];
   float scale_log2;
@@ -1026,7 +1057,11 @@ extern "C" sparsed_status sparsed_attn_paged(const sparsed_cache* cache, int32_t
   p.part_o = reinterpret_cast<float*>(base + at.part_o);
   p.logits = with_mass ? reinterpret_cast<float*>(base + at.logits) : nullptr;
   p.status = static_cast<DeviceStatus*>(ws);
-  cudaError_t e = launch_attn_paged(p, attn_max_ctas() / 2, cache->dtype == SPARSED_DTYPE_FP16, static_cast<cudaStream_t>(cuda_stream));
+  CUtensorMap tk, tv;
+  const CacheView& c = p.cache;
+  if ((st = make_pool_map(&tk, c.k, c.num_pages, cache->page_size, c.heads_kv, c.k_page, c.k_place, c.k_head)) != SPARSED_OK) return st;
+  if ((st = make_pool_map(&tv, c.v, c.num_pages, cache->page_size, c.heads_kv, c.v_page, c.v_place, c.v_head)) != SPARSED_OK) return st;
+  cudaError_t e = launch_attn_paged(tk, tv, p, attn_max_ctas() / 2, cache->dtype == SPARSED_DTYPE_FP16, static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? SPARSED_OK : cuda_fail(e);
 }
 

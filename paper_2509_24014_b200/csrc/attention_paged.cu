@@ -1,24 +1,26 @@
 // Attention of one new token per sequence over a paged key-value cache, head_dim 128, bf16 or fp16, fp32 softmax.
 //
 // Every cached key and value is read once and used for the few query heads of its group only, so HBM bounds it: what matters
-// is that every SM keeps loads in flight all the time, whatever the lengths are. A warp takes 16 keys at a time straight from
-// global memory into the registers that the matrix instructions read, with no shared memory between:
+// is that every SM keeps loads in flight all the time, whatever the lengths are. A warp takes 16 keys at a time: one TMA
+// instruction brings their K (4 KB), one their V, each into a place that only this warp reads, and the next one is issued as
+// soon as the warp has the current one in registers. 16 warps an SM, 128 KB on their way. (Measured on this pattern alone, 2.8
+// GB: TMA 6.9 TB/s with 64 to 192 KB on their way, 16-byte loads into registers 6.8, cp.async 5.2. As loads into registers
+// the whole kernel took 436 us for 24 x 7000 keys x 32 heads, its accumulators leaving no room for the tiles.)
 //   S^T [16 keys x 8 heads]  = K [16 x 128] Q^T: mma.m16n8k16 with K as the A operand. A dot product does not care in which
 //     order it takes head_dim, so a thread's A fragments of two k-steps are one 16-byte piece of a key row, and Q is read with
 //     the same permutation.
-//   O^T [128 x 8 heads] += V^T P^T: V^T as the A operand needs pairs of keys at one d; a thread loads 16-byte pieces of four
+//   O^T [128 x 8 heads] += V^T P^T: V^T as the A operand needs pairs of keys at one d; a thread reads 16-byte pieces of four
 //     keys and pairs them up with byte permutes, d running over the rows of the eight m-tiles in the order that falls out.
 //   P^T is S^T's accumulator turned around in registers (movmatrix).
-// (The fifth-generation tensor instructions read their operands from shared memory and work on 128 rows: with 8 heads, loads
-// into registers need neither staging nor barriers, and the legacy instructions take a tenth of the time the bytes need.)
-// While the next 16 keys' K is on its way the current ones are exponentiated, and the next V while the next S^T is computed:
-// 8 KB of loads per warp, 16 warps per SM (12 with two head tiles), against about 45 KB per SM that 6.5 TB/s need.
+// (The fifth-generation tensor instructions work on 128 rows, with their results in tensor memory and a barrier between each
+// step: with 8 heads the legacy instructions take a tenth of the time the bytes need, and each warp goes at its own pace.)
 //
 // How the work is divided: a unit is 64 keys of one (sequence, key-value head), 16 for each of a CTA's four warps. All units
 // of the call, in order, are dealt out to the CTAs that fit on the device in equal contiguous shares; each CTA finds its own
 // in the lengths. So a long sequence is split over as many CTAs as its share of the work, many short ones share a CTA, and
 // nothing depends on the longest length. A sequence's head that one CTA has from start to end is finished by it; of others,
 // each CTA leaves its part (reference, sum, unnormalised O in fp32), and a second kernel, already waiting, joins the parts.
+// (Smaller shares, taken over by CTAs that are done early, were slower: each costs a start and a part.)
 // That kernel also adds up the keys' attention weights where asked: the first one leaves the logits (4 bytes per head and
 // key against 512 per key), from which p = 2^(logit - LSE) follows once the LSE is known.
 #include "sequences.cuh"
@@ -32,6 +34,7 @@ constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kWarpKeys = 16;
 constexpr int kUnit = kWarps * kWarpKeys;
+constexpr int kTileBytes = kWarpKeys * kHeadDim * 2;
 constexpr int kMostCtas = 1024;
 constexpr float kSlack = 8.f;   // a probability may outgrow its reference to 2^8 before the reference moves
 
@@ -60,34 +63,44 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   return y;
 }
 
-// 16 bytes into four words. (Each byte of the cache is read by one warp only, so it need not stay in L1.)
-__device__ __forceinline__ void load_once(uint32_t* x, const uint16_t* p) {
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "l"(p));
-}
-__device__ __forceinline__ void load_once_if(uint32_t* x, const uint16_t* p, bool wanted) {
-  x[0] = x[1] = x[2] = x[3] = 0u;
-  if (wanted) load_once(x, p);
+__device__ __forceinline__ void load_shared(uint32_t* x, uint32_t from) {
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(from) : "memory");
 }
 
 __device__ __forceinline__ int units_of(int len) { return (len + kUnit - 1) / kUnit; }
 
+// CTAs of the main kernel on an SM, by its registers (128 / 168) and shared memory (54 / 60 KB).
+__host__ __device__ constexpr int ctas_per_sm(int heads) { return heads == 8 ? 4 : 3; }
+
 // kHeads: query heads a CTA works on at once, 8 or 16 (the n-tiles of the matrix instructions).
 template <int kHeads>
 struct PagedSmem {
-  alignas(16) uint16_t q[kHeads][160];   // rows 320 bytes apart: two rows' pieces fall on different banks
+  // K and V of each warp's 16 keys: two 64-wide halves of head_dim, rows of 128 bytes, 128-byte swizzle
+  alignas(1024) uint8_t tiles[kWarps][2][kTileBytes];
+  alignas(16) uint16_t q[2][kHeads][160];   // rows 320 bytes apart: two rows' pieces fall on different banks
+  alignas(16) float o[kWarps][8][kHeadDim + 4];   // of one n-tile
   float m[kWarps][kHeads], l[kWarps][kHeads];
-  alignas(16) float o[kWarps][kHeads][kHeadDim + 4];
-  int thread_units[kThreads];
+  uint64_t full[kWarps][2];
   int warp_units[kWarps];
-  int found_seq, found_units;
+  int found_seq, found_units, found_len;
+  int abort_flag;
 };
 
 template <class Type, int kHeads, bool kMass>
-__global__ void __launch_bounds__(kThreads, kHeads == 8 ? 4 : 3) attn_paged_kernel(const PagedParams p) {
+__global__ void __launch_bounds__(kThreads, ctas_per_sm(kHeads))
+attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const PagedParams p) {
   constexpr int kNT = kHeads / 8;
-  __shared__ PagedSmem<kHeads> sm;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  PagedSmem<kHeads>& sm = *reinterpret_cast<PagedSmem<kHeads>*>(smem_raw);
   wait_for_previous_kernel();
+  if ((smem_u32(smem_raw) & 1023u) != 0u) {
+    if (threadIdx.x == 0) record_status(p.status, 2, 5);
+    return;
+  }
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  // Row g of the 16 x 128 operand K holds key `spread` of its eight, and row g of V^T holds head_dim 8 * spread + j: with this
+  // order neither reading of the swizzled tiles meets a bank conflict.
+  const int spread = (g >> 1) | ((g & 1) << 2);
   const CacheView& c = p.cache;
   const int head_chunks = (p.group + kHeads - 1) / kHeads;
   const int rows = c.heads_kv * head_chunks;   // (key-value head, chunk of its query heads) pairs per sequence
@@ -95,8 +108,11 @@ __global__ void __launch_bounds__(kThreads, kHeads == 8 ? 4 : 3) attn_paged_kern
   // ---- this CTA's share: a scan over the lengths ------------------------------------------------
   const int per_thread = (c.batch + kThreads - 1) / kThreads;
   const int b0 = min(tid * per_thread, c.batch), b1 = min(b0 + per_thread, c.batch);
-  int mine = 0;
-  for (int b = b0; b < b1; ++b) mine += units_of(cached_length(c, b, p.status, 11));
+  int mine = 0, last_len = 0;
+  for (int b = b0; b < b1; ++b) {
+    last_len = cached_length(c, b, p.status, 11);
+    mine += units_of(last_len);
+  }
   int sum = mine;
 #pragma unroll
   for (int d = 1; d < 32; d *= 2) {
@@ -104,6 +120,12 @@ __global__ void __launch_bounds__(kThreads, kHeads == 8 ? 4 : 3) attn_paged_kern
     if (lane >= d) sum += other;
   }
   if (lane == 31) sm.warp_units[warp] = sum;
+  if (tid == 0) {
+    sm.found_seq = sm.found_units = sm.found_len = 0;   // (always found, unless the lengths change under the call)
+    sm.abort_flag = 0;
+  }
+  if (lane < 2) mbar_init(&sm.full[warp][lane], 1);
+  mbar_fence_init();
   __syncthreads();
   int before = sum - mine, total = 0;
 #pragma unroll
@@ -123,56 +145,85 @@ __global__ void __launch_bounds__(kThreads, kHeads == 8 ? 4 : 3) attn_paged_kern
   const int share = (all_units + p.ctas - 1) / p.ctas;
   const int unit0 = static_cast<int>(blockIdx.x) * share, unit1 = min(unit0 + share, all_units);
   if (unit0 >= unit1) return;
-  if (tid == 0) {   // (always found, unless the lengths change under the call)
-    sm.found_seq = 0;
-    sm.found_units = 0;
-  }
-  __syncthreads();
   {
     const int u = unit0 / rows;   // `rows` times a sequence's units lie together, so unit0 is in the sequence that has u
     if (before <= u && u < before + mine) {
       int at = before, b = b0;
-      for (; b < b1; ++b) {
-        const int n = units_of(cached_length(c, b, p.status, 11));
-        if (u < at + n) break;
-        at += n;
+      if (per_thread > 1) {   // (one sequence to a thread: it is at hand)
+        for (; b < b1; ++b) {
+          last_len = cached_length(c, b, p.status, 11);
+          if (u < at + units_of(last_len)) break;
+          at += units_of(last_len);
+        }
       }
       sm.found_seq = b;
       sm.found_units = at;
+      sm.found_len = last_len;
     }
   }
   __syncthreads();
-  int seq = sm.found_seq;
+
+  // ---- the segments of the share: units of one sequence and row each --------------------------------
+  int unit = unit0, seq = sm.found_seq, len = sm.found_len, n_units = units_of(len);
   int seq_unit0 = sm.found_units * rows;   // the sequence's first unit
-
-  const float scale_log2 = p.scale_log2;
+  int tile0 = 0, tile1 = 0, kv_head = 0, head0 = 0, heads = 0;
+  int page = -1, next_page = -1;   // of this warp's keys of units `tile` and `tile` + 1; -1: nothing to do there
+  uint32_t uses = 0;               // tiles this warp has worked on: the phase of its barriers
+  uint32_t buf = 0;                // of Q
   const int place_mask = (1 << c.page_shift) - 1;
-  const int64_t room = static_cast<int64_t>(c.max_pages) << c.page_shift;   // logits per query head
+  const uint32_t k_tile = smem_u32(sm.tiles[warp][0]), v_tile = smem_u32(sm.tiles[warp][1]);
 
-  for (int unit = unit0; unit < unit1;) {
-    // ---- a segment: units of one sequence and row -------------------------------------------
-    int len = cached_length(c, seq, p.status, 11);
-    int n_units = units_of(len);
+  // Positions [key0, key0 + 16) are this warp's of a unit. They lie in one page (page sizes are multiples of 16).
+  auto page_at = [&](int tile) -> int {
+    const int key0 = tile * kUnit + warp * kWarpKeys;
+    return tile < tile1 && key0 < len ? page_of(c, seq, key0 >> c.page_shift, p.status, 12) : -1;
+  };
+  // K (0) or V (1) of this warp's keys in a unit on its way, by one lane, after all lanes have read what was there
+  auto load = [&](int which, int tile, int at_page) {
+    __syncwarp();
+    if (at_page >= 0 && lane == 0) {
+      mbar_expect_tx(&sm.full[warp][which], kTileBytes);
+      tma_load_5d(sm.tiles[warp][which], which == 0 ? &tm_k : &tm_v, &sm.full[warp][which], 0,
+                  (tile * kUnit + warp * kWarpKeys) & place_mask, 0, kv_head, at_page);
+    }
+  };
+  // finds the segment that begins at `unit` and sends its first loads off
+  auto begin_segment = [&]() {
     while (unit >= seq_unit0 + n_units * rows && seq + 1 < c.batch) {   // on to the next sequence that has any
       seq_unit0 += n_units * rows;
       ++seq;
       len = cached_length(c, seq, p.status, 11);
       n_units = units_of(len);
     }
-    if (n_units == 0) break;   // (only if the lengths change under the call)
-    const int row = (unit - seq_unit0) / n_units;
-    const int tile0 = unit - seq_unit0 - row * n_units;
-    const int tile1 = min(n_units, tile0 + unit1 - unit);
-    const int kv_head = row / head_chunks, head0 = kv_head * p.group + (row % head_chunks) * kHeads;
-    const int heads = min(kHeads, p.group - (row % head_chunks) * kHeads);   // of this chunk
-
+    const int row = n_units > 0 ? (unit - seq_unit0) / n_units : 0;
+    tile0 = unit - seq_unit0 - row * n_units;
+    tile1 = min(n_units, tile0 + unit1 - unit);
+    kv_head = row / head_chunks;
+    head0 = kv_head * p.group + (row - kv_head * head_chunks) * kHeads;
+    heads = min(kHeads, (kv_head + 1) * p.group - head0);   // of this chunk
+    page = page_at(tile0);
+    next_page = page_at(tile0 + 1);
     // Q: heads beyond the group's last are zeros
-    for (int i = tid; i < kHeads * 16; i += kThreads) {
-      uint4 x = make_uint4(0u, 0u, 0u, 0u);
-      if ((i >> 4) < heads) x = __ldcg(reinterpret_cast<const uint4*>(p.q + seq * p.q_seq + (head0 + (i >> 4)) * p.q_head + (i & 15) * 8));
-      *reinterpret_cast<uint4*>(&sm.q[i >> 4][(i & 15) * 8]) = x;
+    constexpr int kPieces = kHeads * 16 / kThreads;
+    uint4 qx[kPieces];
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x) {
+      const int i = x * kThreads + tid;
+      qx[x] = make_uint4(0u, 0u, 0u, 0u);
+      if ((i >> 4) < heads) qx[x] = __ldcg(reinterpret_cast<const uint4*>(p.q + seq * p.q_seq + (head0 + (i >> 4)) * p.q_head + (i & 15) * 8));
     }
+    load(0, tile0, page);
+    load(1, tile0, page);
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x) {
+      const int i = x * kThreads + tid;
+      *reinterpret_cast<uint4*>(&sm.q[buf][i >> 4][(i & 15) * 8]) = qx[x];
+    }
+  };
 
+  begin_segment();
+  bool ok = true;
+  while (true) {
     float o[kNT][8][4];
     float m[kNT][2], l[kNT][2];
 #pragma unroll
@@ -184,86 +235,48 @@ __global__ void __launch_bounds__(kThreads, kHeads == 8 ? 4 : 3) attn_paged_kern
       m[n][0] = m[n][1] = -INFINITY;
       l[n][0] = l[n][1] = 0.f;
     }
-    uint32_t kx[2][16], vx[4][8];   // K: rows g and g + 8, pieces 4 i + t; V: keys 2t, 2t + 1, 2t + 8, 2t + 9, pieces g and g + 8
-    // Positions [key0, key0 + 16) are this warp's of a unit. They lie in one page (page sizes are multiples of 16).
-    auto page_at = [&](int tile) -> int {
-      const int key0 = tile * kUnit + warp * kWarpKeys;
-      return tile < tile1 && key0 < len ? page_of(c, seq, key0 >> c.page_shift, p.status, 12) : -1;
-    };
-    const uint16_t* k_lane = c.k + kv_head * c.k_head + g * c.k_place + t * 8;
-    const uint16_t* v_lane = c.v + kv_head * c.v_head + 2 * t * c.v_place + g * 8;
-    // K and V of the warp's keys in a unit; positions at and beyond `valid` are not read: zeros
-    auto load_k = [&](int page, int key0, int valid) {
-      const uint16_t* k = k_lane + page * c.k_page + (key0 & place_mask) * c.k_place;
-      if (valid >= kWarpKeys) {
-#pragma unroll
-        for (int r = 0; r < 2; ++r, k += 8 * c.k_place)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) load_once(kx[r] + 4 * i, k + i * 32);
-      } else {
-#pragma unroll
-        for (int r = 0; r < 2; ++r, k += 8 * c.k_place)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) load_once_if(kx[r] + 4 * i, k + i * 32, g + 8 * r < valid);
-      }
-    };
-    auto load_v = [&](int page, int key0, int valid) {
-      const uint16_t* v = v_lane + page * c.v_page + (key0 & place_mask) * c.v_place;
-      if (valid >= kWarpKeys) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r, v += (r == 2 ? 7 : 1) * c.v_place) {   // keys 2t, 2t + 1, 2t + 8, 2t + 9
-          load_once(vx[r], v);
-          load_once(vx[r] + 4, v + 64);
-        }
-      } else {
-#pragma unroll
-        for (int r = 0; r < 4; ++r, v += (r == 2 ? 7 : 1) * c.v_place) {
-          const bool wanted = 2 * t + (r & 1) + 8 * (r >> 1) < valid;
-          load_once_if(vx[r], v, wanted);
-          load_once_if(vx[r] + 4, v + 64, wanted);
-        }
-      }
-    };
-    // valid keys of this warp in a unit: none where there is no page
-    auto valid_at = [&](int tile, int page) -> int { return page < 0 ? 0 : len - tile * kUnit - warp * kWarpKeys; };
-
-    int page = page_at(tile0);
-    int valid = valid_at(tile0, page);
-    load_k(page, tile0 * kUnit + warp * kWarpKeys, valid);
-    load_v(page, tile0 * kUnit + warp * kWarpKeys, valid);
-    int next_page = page_at(tile0 + 1);
-    [[maybe_unused]] float* logits = nullptr;   // of key 0 + g, head 2t
-    if constexpr (kMass)
-      logits = p.logits + (static_cast<int64_t>(seq) * c.heads_kv * p.group + head0 + 2 * t) * room + g;
+    const int64_t room = static_cast<int64_t>(c.max_pages) << c.page_shift;   // logits per query head
+    [[maybe_unused]] float* logits = nullptr;   // of key `spread`, head 2t
+    if constexpr (kMass) logits = p.logits + (static_cast<int64_t>(seq) * c.heads_kv * p.group + head0 + 2 * t) * room + spread;
     __syncthreads();   // Q is there
     for (int tile = tile0; tile < tile1; ++tile) {
       const int key0 = tile * kUnit + warp * kWarpKeys;
-      const int next_valid = valid_at(tile + 1, next_page);
-      // ---- S^T = K Q^T, in two chains of dependent instructions
-      float s[kNT][4];
-#pragma unroll
-      for (int n = 0; n < kNT; ++n) {
-        float s2[4] = {0.f, 0.f, 0.f, 0.f};
-        s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint4 q = *reinterpret_cast<const uint4*>(&sm.q[n * 8 + g][(4 * i + t) * 8]);
-          mma16816<Type>(s[n], kx[0][4 * i], kx[1][4 * i], kx[0][4 * i + 1], kx[1][4 * i + 1], q.x, q.y);
-          mma16816<Type>(s2, kx[0][4 * i + 2], kx[1][4 * i + 2], kx[0][4 * i + 3], kx[1][4 * i + 3], q.z, q.w);
-        }
-#pragma unroll
-        for (int x = 0; x < 4; ++x) s[n][x] = (s[n][x] + s2[x]) * scale_log2;
-      }
-      if (tile + 1 < tile1) load_k(next_page, key0 + kUnit, next_valid);
       const int page_after = page_at(tile + 2);
-      // ---- probabilities
-      if (valid > 0) {   // (the same for the whole warp)
+      if (page >= 0) {   // (the same for the whole warp; false: no keys, or no page)
+        // ---- S^T = K Q^T, in two chains of dependent instructions
+        float s[kNT][4];
+        {
+          ok = mbar_wait(&sm.full[warp][0], uses & 1, &sm.abort_flag, p.status, 15);
+          if (!(ok = __all_sync(0xffffffffu, ok))) break;
+          uint32_t kx[2][16];   // rows g and g + 8, pieces 4 i + t
+          const uint32_t at = k_tile + spread * 128 + ((t ^ spread) << 4);
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load_shared(kx[r] + 4 * i, (at ^ ((i & 1) << 6)) + r * 1024 + (i >> 1) * 2048);
+          load(0, tile + 1, next_page);
+#pragma unroll
+          for (int n = 0; n < kNT; ++n) {
+            float s2[4] = {0.f, 0.f, 0.f, 0.f};
+            s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint4 q = *reinterpret_cast<const uint4*>(&sm.q[buf][n * 8 + g][(4 * i + t) * 8]);
+              mma16816<Type>(s[n], kx[0][4 * i], kx[1][4 * i], kx[0][4 * i + 1], kx[1][4 * i + 1], q.x, q.y);
+              mma16816<Type>(s2, kx[0][4 * i + 2], kx[1][4 * i + 2], kx[0][4 * i + 3], kx[1][4 * i + 3], q.z, q.w);
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) s[n][x] = (s[n][x] + s2[x]) * p.scale_log2;
+          }
+        }
+        // ---- probabilities
+        const int valid = len - key0;
         if (valid < kWarpKeys) {
 #pragma unroll
           for (int n = 0; n < kNT; ++n)
 #pragma unroll
             for (int x = 0; x < 4; ++x)
-              if (g + 8 * (x >> 1) >= valid) s[n][x] = -INFINITY;
+              if (spread + 8 * (x >> 1) >= valid) s[n][x] = -INFINITY;
         }
         bool outgrown = false;
 #pragma unroll
@@ -275,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, kHeads == 8 ? 4 : 3) attn_paged_kern
           for (int n = 0; n < kNT; ++n)
 #pragma unroll
             for (int x = 0; x < 4; ++x)
-              if (8 * n + 2 * t + (x & 1) < heads && g + 8 * (x >> 1) < valid)
+              if (8 * n + 2 * t + (x & 1) < heads && spread + 8 * (x >> 1) < valid)
                 logits[(8 * n + (x & 1)) * room + key0 + 8 * (x >> 1)] = s[n][x];
         }
         if (__any_sync(0xffffffffu, outgrown)) {
@@ -300,7 +313,7 @@ __global__ void __launch_bounds__(kThreads, kHeads == 8 ? 4 : 3) attn_paged_kern
               }
             }
         }
-        uint32_t pt[kNT][2];   // P^T as the B operand: keys 2t, 2t + 1 / 2t + 8, 2t + 9 of head g
+        uint32_t pt[kNT][2];   // P^T as the B operand: rows 2t, 2t + 1 / 2t + 8, 2t + 9 of S^T, head g
 #pragma unroll
         for (int n = 0; n < kNT; ++n) {
           float e[4];
@@ -313,7 +326,24 @@ __global__ void __launch_bounds__(kThreads, kHeads == 8 ? 4 : 3) attn_paged_kern
           pt[n][0] = transpose8x8(Type::pack(e[0], e[1]));
           pt[n][1] = transpose8x8(Type::pack(e[2], e[3]));
         }
-        // ---- O^T += V^T P^T
+        // ---- O^T += V^T P^T. Rows 2t, 2t + 1, 2t + 8, 2t + 9 of S^T are keys t, t + 4, t + 8, t + 12.
+        ok = mbar_wait(&sm.full[warp][1], uses & 1, &sm.abort_flag, p.status, 16);
+        if (!(ok = __all_sync(0xffffffffu, ok))) break;
+        uint32_t vx[4][8];   // pieces `spread` and `spread` + 8 of the four keys
+        const uint32_t at = v_tile + t * 128 + ((spread ^ t) << 4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) load_shared(vx[r] + 4 * i, (at ^ ((r & 1) << 6)) + r * 512 + i * 2048);
+        load(1, tile + 1, next_page);
+        if (valid < kWarpKeys) {   // what lies behind the sequence may be anything, and 0 * NaN is NaN
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (t + 4 * r >= valid) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) vx[r][i] = 0u;
+            }
+        }
 #pragma unroll
         for (int w = 0; w < 4; ++w)
 #pragma unroll
@@ -324,16 +354,35 @@ __global__ void __launch_bounds__(kThreads, kHeads == 8 ? 4 : 3) attn_paged_kern
 #pragma unroll
             for (int n = 0; n < kNT; ++n) mma16816<Type>(o[n][2 * w + odd], a0, a1, a2, a3, pt[n][0], pt[n][1]);
           }
+        ++uses;
+      } else {
+        load(0, tile + 1, next_page);
+        load(1, tile + 1, next_page);
+        if constexpr (kMass) {   // keys without a page have no weight
+#pragma unroll
+          for (int n = 0; n < kNT; ++n)
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              if (8 * n + 2 * t + (x & 1) < heads && key0 + spread + 8 * (x >> 1) < len)
+                logits[(8 * n + (x & 1)) * room + key0 + 8 * (x >> 1)] = -INFINITY;
+        }
       }
-      if (tile + 1 < tile1) load_v(next_page, key0 + kUnit, next_valid);
-      valid = next_valid;
+      page = next_page;
       next_page = page_after;
     }
+    if (!__syncthreads_and(ok)) break;   // (a wait has run out)
 
-    // ---- the four warps' shares together -----------------------------------------------------
-    // o[n][j]: d = 8 g + j (0, 1) and 64 + 8 g + j (2, 3) of heads 2t and 2t + 1 of n-tile n
+    // ---- the next segment's first loads on their way, then the four warps' shares of this one together ---------
+    const bool whole = tile0 == 0 && tile1 == n_units;
+    const int slot = 2 * static_cast<int>(blockIdx.x) + (tile0 == 0 ? 1 : 0);
+    const int done_seq = seq, done_head0 = head0, done_heads = heads;
+    unit += tile1 - tile0;
+    buf ^= 1;
+    if (unit < unit1) begin_segment();
+    // o[n][j]: d = 8 * spread + j (0, 1) and 64 + 8 * spread + j (2, 3) of heads 2t and 2t + 1 of n-tile n
 #pragma unroll
-    for (int n = 0; n < kNT; ++n)
+    for (int n = 0; n < kNT; ++n) {
+      if (n > 0) __syncthreads();   // the n-tile before has been read
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         l[n][x] += __shfl_xor_sync(0xffffffffu, l[n][x], 4);
@@ -344,54 +393,59 @@ __global__ void __launch_bounds__(kThreads, kHeads == 8 ? 4 : 3) attn_paged_kern
           sm.m[warp][h] = m[n][x];
           sm.l[warp][h] = l[n][x];
         }
-        float4* low = reinterpret_cast<float4*>(&sm.o[warp][h][8 * g]);
-        float4* high = reinterpret_cast<float4*>(&sm.o[warp][h][64 + 8 * g]);
+        float4* low = reinterpret_cast<float4*>(&sm.o[warp][2 * t + x][8 * spread]);
+        float4* high = reinterpret_cast<float4*>(&sm.o[warp][2 * t + x][64 + 8 * spread]);
         low[0] = make_float4(o[n][0][x], o[n][1][x], o[n][2][x], o[n][3][x]);
         low[1] = make_float4(o[n][4][x], o[n][5][x], o[n][6][x], o[n][7][x]);
         high[0] = make_float4(o[n][0][x + 2], o[n][1][x + 2], o[n][2][x + 2], o[n][3][x + 2]);
         high[1] = make_float4(o[n][4][x + 2], o[n][5][x + 2], o[n][6][x + 2], o[n][7][x + 2]);
       }
-    __syncthreads();
-    const bool whole = tile0 == 0 && tile1 == n_units;
-    const int slot = 2 * static_cast<int>(blockIdx.x) + (tile0 == 0 ? 1 : 0);
-    for (int h = 0; h < heads; ++h) {
-      float top = sm.m[0][h];
+      __syncthreads();
+      for (int h = 8 * n; h < min(8 * n + 8, done_heads); ++h) {
+        float top = sm.m[0][h];
 #pragma unroll
-      for (int w = 1; w < kWarps; ++w) top = fmaxf(top, sm.m[w][h]);
-      const float ref = top == -INFINITY ? 0.f : top;
-      float sum_l = 0.f, sum_o = 0.f;
+        for (int w = 1; w < kWarps; ++w) top = fmaxf(top, sm.m[w][h]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        float sum_l = 0.f, sum_o = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float f = fast_exp2(sm.m[w][h] - ref);
-        sum_l += f * sm.l[w][h];
-        sum_o += f * sm.o[w][h][tid];
-      }
-      if (whole) {
-        const float inv = sum_l == 0.f ? 0.f : 1.f / sum_l;   // (0: every page was missing)
-        p.o[seq * p.o_seq + (head0 + h) * p.o_head + tid] = static_cast<uint16_t>(Type::pack(sum_o * inv, 0.f) & 0xffffu);
-        if (tid == 0) {
-          const float lse2 = top + log2f(sum_l);
-          p.lse2[static_cast<int64_t>(seq) * c.heads_kv * p.group + head0 + h] = lse2;
-          if (p.lse != nullptr) p.lse[static_cast<int64_t>(seq) * c.heads_kv * p.group + head0 + h] = lse2 * 0.69314718055994531f;
+        for (int w = 0; w < kWarps; ++w) {
+          const float f = fast_exp2(sm.m[w][h] - ref);
+          sum_l += f * sm.l[w][h];
+          sum_o += f * sm.o[w][h - 8 * n][tid];
         }
-      } else {
-        p.part_o[(static_cast<int64_t>(slot) * kHeads + h) * kHeadDim + tid] = sum_o;
-        if (tid == 0) p.part_ml[slot * kHeads + h] = make_float2(top, sum_l);
+        if (whole) {
+          const float inv = sum_l == 0.f ? 0.f : 1.f / sum_l;   // (0: every page was missing)
+          p.o[done_seq * p.o_seq + (done_head0 + h) * p.o_head + tid] = static_cast<uint16_t>(Type::pack(sum_o * inv, 0.f) & 0xffffu);
+          if (tid == 0) {
+            const float lse2 = top + log2f(sum_l);
+            p.lse2[static_cast<int64_t>(done_seq) * c.heads_kv * p.group + done_head0 + h] = lse2;
+            if (p.lse != nullptr) p.lse[static_cast<int64_t>(done_seq) * c.heads_kv * p.group + done_head0 + h] = lse2 * 0.69314718055994531f;
+          }
+        } else {
+          p.part_o[(static_cast<int64_t>(slot) * kHeads + h) * kHeadDim + tid] = sum_o;
+          if (tid == 0) p.part_ml[slot * kHeads + h] = make_float2(top, sum_l);
+        }
       }
     }
-    __syncthreads();   // the next segment overwrites Q and the shares
-    unit += tile1 - tile0;
+    // (the shares are read before any warp writes the next segment's: two barriers lie between)
+    if (unit >= unit1) return;
   }
+  // Given up: what is on its way must have landed before the CTA leaves (bounded like every wait).
+  for (int which = 0; which < 2; ++which)
+    for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(&sm.full[warp][which], uses & 1); ++i) {
+    }
 }
 
 // ------------------------------------------------------------------------------------------
 // The parts of split sequences together, and the keys' weights. Blocks [0, heads_q) of a sequence finish one query head each;
 // with weights, the others take kMassKeys keys of one key-value head each.
 // ------------------------------------------------------------------------------------------
-constexpr int kJoinThreads = 128;
+constexpr int kJoinThreads = 256;
+constexpr int kJoinBatch = 4;   // parts that a warp reads at once
 constexpr int kMassKeys = 1024;
+constexpr int kMassHeads = 8;   // whose logits a thread has in flight
 
-template <class Type, int kHeads>
+template <class Type, int kHeads, bool kMass>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p, int blocks_per_seq, int mass_blocks) {
   __shared__ float2 warp_ml[kJoinThreads / 32];
   __shared__ float4 warp_o[kJoinThreads / 32][32];
@@ -416,29 +470,48 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p,
     const int head = what, in_chunk = head % p.group % kHeads;
     uint16_t* o = p.o + seq * p.o_seq + head * p.o_head;
     if (n_units == 0) {
-      o[tid] = 0;
+      if (tid < kHeadDim) o[tid] = 0;
       if (p.lse != nullptr && tid == 0) p.lse[static_cast<int64_t>(seq) * heads_q + head] = -INFINITY;
       return;
     }
     const int2 ctas = ctas_of(head);
     if (ctas.x == ctas.y) return;   // finished already
-    // each warp takes every fourth part; a lane has four numbers of the output
+    // Warps take the parts in turn, four at a time, a lane four numbers of the output: all loads of a batch at once.
+    const int parts = ctas.y - ctas.x + 1;
     float m = -INFINITY, l = 0.f;
     float4 o4 = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int cta = ctas.x + warp; cta <= ctas.y; cta += kJoinThreads / 32) {
-      const int64_t at = slot_of(cta, ctas) * kHeads + in_chunk;
-      const float2 ml = __ldcg(p.part_ml + at);
-      const float4 x = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * kHeadDim) + lane);
-      const float top = fmaxf(m, ml.x), ref = top == -INFINITY ? 0.f : top;
-      const float a = fast_exp2(m - ref), b = fast_exp2(ml.x - ref);
+    for (int i0 = warp; i0 < parts; i0 += kJoinBatch * kJoinThreads / 32) {
+      float2 ml[kJoinBatch];
+      float4 x[kJoinBatch];
+      float top = m;
+#pragma unroll
+      for (int j = 0; j < kJoinBatch; ++j) {
+        const int i = i0 + j * kJoinThreads / 32;
+        ml[j] = make_float2(-INFINITY, 0.f);
+        x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i < parts) {
+          const int64_t at = slot_of(ctas.x + i, ctas) * kHeads + in_chunk;
+          ml[j] = __ldcg(p.part_ml + at);
+          x[j] = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * kHeadDim) + lane);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kJoinBatch; ++j) top = fmaxf(top, ml[j].x);
+      const float ref = top == -INFINITY ? 0.f : top, a = fast_exp2(m - ref);
       m = top;
-      l = l * a + ml.y * b;
-      o4 = make_float4(o4.x * a + x.x * b, o4.y * a + x.y * b, o4.z * a + x.z * b, o4.w * a + x.w * b);
+      l *= a;
+      o4 = make_float4(o4.x * a, o4.y * a, o4.z * a, o4.w * a);
+#pragma unroll
+      for (int j = 0; j < kJoinBatch; ++j) {
+        const float f = fast_exp2(ml[j].x - ref);
+        l += f * ml[j].y;
+        o4 = make_float4(o4.x + f * x[j].x, o4.y + f * x[j].y, o4.z + f * x[j].z, o4.w + f * x[j].w);
+      }
     }
     if (lane == 0) warp_ml[warp] = make_float2(m, l);
     warp_o[warp][lane] = o4;
     __syncthreads();
+    if (tid >= kHeadDim) return;
     float top = warp_ml[0].x;
 #pragma unroll
     for (int w = 1; w < kJoinThreads / 32; ++w) top = fmaxf(top, warp_ml[w].x);
@@ -455,10 +528,35 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p,
     if (p.lse != nullptr && tid == 0) p.lse[static_cast<int64_t>(seq) * heads_q + head] = (top + log2f(sum_l)) * 0.69314718055994531f;
     return;
   }
+  if constexpr (!kMass) return;
   // ---- weights of keys [key0, key0 + kMassKeys) of one key-value head
   const int kv_head = (what - heads_q) / mass_blocks, key0 = (what - heads_q) % mass_blocks * kMassKeys;
   const int len = cached_length(c, seq, p.status, 13);
   if (key0 >= len) return;
+  // The first heads' logits are on their way while the heads' LSE is worked out. (A key whose page is missing has -inf there.)
+  const int64_t row = static_cast<int64_t>(seq) * c.heads_kv + kv_head;
+  const int64_t room = static_cast<int64_t>(c.max_pages) << c.page_shift;
+  const float* logits = p.logits + row * p.group * room;
+  float x[kMassHeads][kMassKeys / kJoinThreads], sum[kMassKeys / kJoinThreads];
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int h = 0; h < kMassHeads; ++h)
+#pragma unroll
+      for (int i = 0; i < kMassKeys / kJoinThreads; ++i) {
+        const int j = key0 + i * kJoinThreads + tid;
+        x[h][i] = h0 + h < p.group && j < len ? __ldcg(logits + (h0 + h) * room + j) : 0.f;
+      }
+  };
+  auto add = [&](int h, float lse2) {
+#pragma unroll
+    for (int i = 0; i < kMassKeys / kJoinThreads; ++i) sum[i] += fast_exp2(x[h][i] - lse2);
+  };
+#pragma unroll
+  for (int i = 0; i < kMassKeys / kJoinThreads; ++i) {
+    const int j = key0 + i * kJoinThreads + tid;
+    sum[i] = p.mass_in != nullptr && j < len ? __ldcg(p.mass_in + row * p.mass_capacity + j) : 0.f;
+  }
+  load(0);
   for (int h = warp; h < p.group; h += kJoinThreads / 32) {
     const int head = kv_head * p.group + h;
     const int2 ctas = ctas_of(head);
@@ -482,33 +580,46 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p,
       for (int d = 16; d > 0; d /= 2) l += __shfl_xor_sync(0xffffffffu, l, d);
       lse2 = top + log2f(l);
     }
-    if (lane == 0) lse_of[h] = lse2;
+    if (lane == 0) lse_of[h] = lse2 == -INFINITY ? 0.f : lse2;   // (no key at all: 2^(-inf - 0) = 0)
   }
   __syncthreads();
-  const int64_t row = static_cast<int64_t>(seq) * c.heads_kv + kv_head;
-  const int64_t room = static_cast<int64_t>(c.max_pages) << c.page_shift;
-  const float* logits = p.logits + row * p.group * room;
-  for (int j = key0 + tid; j < min(key0 + kMassKeys, len); j += kJoinThreads) {
-    float sum = 0.f;
-    const int page = page_of(c, seq, j >> c.page_shift, p.status, 12);   // (a key whose page is missing has no weight)
-    if (page >= 0)
-      for (int h = 0; h < p.group; ++h) sum += fast_exp2(__ldcg(logits + h * room + j) - lse_of[h]);
-    const float had = p.mass_in != nullptr ? __ldcg(p.mass_in + row * p.mass_capacity + j) : 0.f;
-    p.mass_out[row * p.mass_capacity + j] = had + sum;
+#pragma unroll
+  for (int h = 0; h < kMassHeads; ++h)
+    if (h < p.group) add(h, lse_of[h]);
+  for (int h0 = kMassHeads; h0 < p.group; h0 += kMassHeads) {
+    load(h0);
+#pragma unroll
+    for (int h = 0; h < kMassHeads; ++h)
+      if (h0 + h < p.group) add(h, lse_of[h0 + h]);
+  }
+#pragma unroll
+  for (int i = 0; i < kMassKeys / kJoinThreads; ++i) {
+    const int j = key0 + i * kJoinThreads + tid;
+    if (j < len) p.mass_out[row * p.mass_capacity + j] = sum[i];
   }
 }
 
 template <class Type, int kHeads>
-cudaError_t launch(const PagedParams& p, cudaStream_t stream) {
-  cudaError_t e = p.mass_out != nullptr
-                      ? launch_overlapped(attn_paged_kernel<Type, kHeads, true>, p.ctas, p.ctas, kThreads, 0, stream, p)
-                      : launch_overlapped(attn_paged_kernel<Type, kHeads, false>, p.ctas, p.ctas, kThreads, 0, stream, p);
+cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const PagedParams& p, bool full, cudaStream_t stream) {
+  const bool mass = p.mass_out != nullptr;
+  auto kernel = mass ? attn_paged_kernel<Type, kHeads, true> : attn_paged_kernel<Type, kHeads, false>;
+  const int smem = static_cast<int>(sizeof(PagedSmem<kHeads>));
+  static_assert(ctas_per_sm(kHeads) * (sizeof(PagedSmem<kHeads>) + 1024) <= 228 * 1024, "CTAs per SM");
+  static SmemLimit limits[2];
+  cudaError_t e = ensure_dynamic_smem(kernel, smem, limits[mass ? 1 : 0]);
+  if (e != cudaSuccess) return e;
+  e = launch_overlapped(kernel, p.ctas, p.ctas, kThreads, smem, stream, tk, tv, p);
   if (e != cudaSuccess) return e;
   const int room = p.cache.max_pages << p.cache.page_shift;
   const int mass_blocks = p.mass_out != nullptr ? (room + kMassKeys - 1) / kMassKeys : 0;
   const int blocks_per_seq = p.cache.heads_kv * (p.group + mass_blocks);
   const long long blocks = static_cast<long long>(blocks_per_seq) * p.cache.batch;
-  return launch_overlapped(join_kernel<Type, kHeads>, blocks, blocks, kJoinThreads, p.group * sizeof(float), stream, p, blocks_per_seq, mass_blocks);
+  // The joining kernel is overlapped with a main kernel that leaves SMs free. Where that fills the device, the next call's
+  // main kernel, overlapped in its turn, would find SMs with the joining CTAs still on them and be placed unevenly (24 x 7000
+  // keys x 32 heads, calls back to back: 508 us against 417).
+  const long long room_for = full ? 0 : blocks;
+  return mass ? launch_overlapped(join_kernel<Type, kHeads, true>, blocks, room_for, kJoinThreads, p.group * sizeof(float), stream, p, blocks_per_seq, mass_blocks)
+              : launch_overlapped(join_kernel<Type, kHeads, false>, blocks, room_for, kJoinThreads, 0, stream, p, blocks_per_seq, 0);
 }
 
 int heads_at_once(int group) { return group <= 8 ? 8 : 16; }
@@ -535,13 +646,14 @@ PagedLayout paged_layout(int batch, int heads_kv, int group, int max_pages, int 
   return at;
 }
 
-cudaError_t launch_attn_paged(PagedParams p, int sms, bool fp16, cudaStream_t stream) {
+cudaError_t launch_attn_paged(const CUtensorMap& tk, const CUtensorMap& tv, PagedParams p, int sms, bool fp16, cudaStream_t stream) {
   const int heads = heads_at_once(p.group);
-  const int fit = sms * (heads == 8 ? 4 : 3);
+  const int fit = sms * ctas_per_sm(heads);
   const int most = paged_max_ctas(p.cache.batch, p.cache.heads_kv, p.group, p.cache.max_pages, 1 << p.cache.page_shift);
-  p.ctas = fit < most ? fit : most;
-  if (heads == 8) return fp16 ? launch<Fp16Type, 8>(p, stream) : launch<Bf16Type, 8>(p, stream);
-  return fp16 ? launch<Fp16Type, 16>(p, stream) : launch<Bf16Type, 16>(p, stream);
+  const bool full = fit <= most;
+  p.ctas = full ? fit : most;
+  if (heads == 8) return fp16 ? launch<Fp16Type, 8>(tk, tv, p, full, stream) : launch<Bf16Type, 8>(tk, tv, p, full, stream);
+  return fp16 ? launch<Fp16Type, 16>(tk, tv, p, full, stream) : launch<Bf16Type, 16>(tk, tv, p, full, stream);
 }
 
 }  // namespace sparsed

@@ -74,7 +74,9 @@ struct PagedLayout {
 };
 PagedLayout paged_layout(int batch, int heads_kv, int group, int max_pages, int page_size, bool with_mass);
 int paged_max_ctas(int batch, int heads_kv, int group, int max_pages, int page_size);   // the layout's bound on `ctas`
-cudaError_t launch_attn_paged(PagedParams p, int sms, bool fp16, cudaStream_t stream);
+// (tensor maps of K and V: [pages, heads, 2, places, 64] with the two halves of head_dim apart, boxes of 64 x 16 places x 2)
+cudaError_t launch_attn_paged(const CUtensorMap& tk, const CUtensorMap& tv, PagedParams p, int sms, bool fp16,
+                              cudaStream_t stream);
 
 struct EvictParams {
   CacheView from, to;
