@@ -171,6 +171,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   uint32_t uses = 0;               // tiles this warp has worked on: the phase of its barriers
   uint32_t buf = 0;                // of Q
   const int place_mask = (1 << c.page_shift) - 1;
+  const uint64_t once = l2_evict_first();   // (so that the logits and parts for the joining kernel stay in L2)
   const uint32_t k_tile = smem_u32(sm.tiles[warp][0]), v_tile = smem_u32(sm.tiles[warp][1]);
 
   // Positions [key0, key0 + 16) are this warp's of a unit. They lie in one page (page sizes are multiples of 16).
@@ -184,7 +185,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     if (at_page >= 0 && lane == 0) {
       mbar_expect_tx(&sm.full[warp][which], kTileBytes);
       tma_load_5d(sm.tiles[warp][which], which == 0 ? &tm_k : &tm_v, &sm.full[warp][which], 0,
-                  (tile * kUnit + warp * kWarpKeys) & place_mask, 0, kv_head, at_page);
+                  (tile * kUnit + warp * kWarpKeys) & place_mask, 0, kv_head, at_page, once);
     }
   };
   // finds the segment that begins at `unit` and sends its first loads off
@@ -442,7 +443,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 // ------------------------------------------------------------------------------------------
 constexpr int kJoinThreads = 256;
 constexpr int kJoinBatch = 4;   // parts that a warp reads at once
-constexpr int kMassKeys = 1024;
+constexpr int kMassKeys = 4 * kJoinThreads;
 constexpr int kMassHeads = 8;   // whose logits a thread has in flight
 
 template <class Type, int kHeads, bool kMass>
@@ -537,24 +538,37 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p,
   const int64_t row = static_cast<int64_t>(seq) * c.heads_kv + kv_head;
   const int64_t room = static_cast<int64_t>(c.max_pages) << c.page_shift;
   const float* logits = p.logits + row * p.group * room;
-  float x[kMassHeads][kMassKeys / kJoinThreads], sum[kMassKeys / kJoinThreads];
+  // four consecutive keys to a thread (rows of logits are whole numbers of 64 bytes)
+  const int j = key0 + 4 * tid;
+  const float* at = logits + j;
+  float4 x[kMassHeads], sum = make_float4(0.f, 0.f, 0.f, 0.f);
   auto load = [&](int h0) {
 #pragma unroll
-    for (int h = 0; h < kMassHeads; ++h)
-#pragma unroll
-      for (int i = 0; i < kMassKeys / kJoinThreads; ++i) {
-        const int j = key0 + i * kJoinThreads + tid;
-        x[h][i] = h0 + h < p.group && j < len ? __ldcg(logits + (h0 + h) * room + j) : 0.f;
-      }
+    for (int h = 0; h < kMassHeads; ++h) {
+      x[h] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (h0 + h < p.group && j < len) x[h] = __ldcg(reinterpret_cast<const float4*>(at + (h0 + h) * room));
+    }
   };
-  auto add = [&](int h, float lse2) {
-#pragma unroll
-    for (int i = 0; i < kMassKeys / kJoinThreads; ++i) sum[i] += fast_exp2(x[h][i] - lse2);
+  auto add = [&](float4 v, float lse2) {
+    sum.x += fast_exp2(v.x - lse2);
+    sum.y += fast_exp2(v.y - lse2);
+    sum.z += fast_exp2(v.z - lse2);
+    sum.w += fast_exp2(v.w - lse2);
   };
-#pragma unroll
-  for (int i = 0; i < kMassKeys / kJoinThreads; ++i) {
-    const int j = key0 + i * kJoinThreads + tid;
-    sum[i] = p.mass_in != nullptr && j < len ? __ldcg(p.mass_in + row * p.mass_capacity + j) : 0.f;
+  const float* had = p.mass_in != nullptr ? p.mass_in + row * p.mass_capacity + j : nullptr;
+  float* to = p.mass_out + row * p.mass_capacity + j;
+  const bool vector = j + 4 <= len && p.mass_capacity % 4 == 0 &&
+                      ((reinterpret_cast<uintptr_t>(p.mass_in) | reinterpret_cast<uintptr_t>(p.mass_out)) & 15) == 0;
+  float4 before = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (had != nullptr) {
+    if (vector) {
+      before = __ldcg(reinterpret_cast<const float4*>(had));
+    } else {
+      if (j < len) before.x = __ldcg(had);
+      if (j + 1 < len) before.y = __ldcg(had + 1);
+      if (j + 2 < len) before.z = __ldcg(had + 2);
+      if (j + 3 < len) before.w = __ldcg(had + 3);
+    }
   }
   load(0);
   for (int h = warp; h < p.group; h += kJoinThreads / 32) {
@@ -585,17 +599,21 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p,
   __syncthreads();
 #pragma unroll
   for (int h = 0; h < kMassHeads; ++h)
-    if (h < p.group) add(h, lse_of[h]);
+    if (h < p.group) add(x[h], lse_of[h]);
   for (int h0 = kMassHeads; h0 < p.group; h0 += kMassHeads) {
     load(h0);
 #pragma unroll
     for (int h = 0; h < kMassHeads; ++h)
-      if (h0 + h < p.group) add(h, lse_of[h0 + h]);
+      if (h0 + h < p.group) add(x[h], lse_of[h0 + h]);
   }
-#pragma unroll
-  for (int i = 0; i < kMassKeys / kJoinThreads; ++i) {
-    const int j = key0 + i * kJoinThreads + tid;
-    if (j < len) p.mass_out[row * p.mass_capacity + j] = sum[i];
+  // (the last keys' neighbours in the row of logits may hold anything: they are not stored)
+  if (vector) {
+    *reinterpret_cast<float4*>(to) = make_float4(before.x + sum.x, before.y + sum.y, before.z + sum.z, before.w + sum.w);
+  } else {
+    if (j < len) to[0] = before.x + sum.x;
+    if (j + 1 < len) to[1] = before.y + sum.y;
+    if (j + 2 < len) to[2] = before.z + sum.z;
+    if (j + 3 < len) to[3] = before.w + sum.w;
   }
 }
 
