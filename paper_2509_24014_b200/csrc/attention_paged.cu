@@ -441,8 +441,8 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 // The parts of split sequences together, and the keys' weights. Blocks [0, heads_q) of a sequence finish one query head each;
 // with weights, the others take kMassKeys keys of one key-value head each.
 // ------------------------------------------------------------------------------------------
-constexpr int kJoinThreads = 256;
-constexpr int kJoinBatch = 4;   // parts that a warp reads at once
+constexpr int kJoinThreads = 128;
+constexpr int kJoinBatch = 8;   // parts that a warp reads at once
 constexpr int kMassKeys = 4 * kJoinThreads;
 constexpr int kMassHeads = 8;   // whose logits a thread has in flight
 
@@ -477,7 +477,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p,
     }
     const int2 ctas = ctas_of(head);
     if (ctas.x == ctas.y) return;   // finished already
-    // Warps take the parts in turn, four at a time, a lane four numbers of the output: all loads of a batch at once.
+    // Warps take the parts in turn, eight at a time, a lane four numbers of the output: all loads of a batch at once.
     const int parts = ctas.y - ctas.x + 1;
     float m = -INFINITY, l = 0.f;
     float4 o4 = make_float4(0.f, 0.f, 0.f, 0.f);
