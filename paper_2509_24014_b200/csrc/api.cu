@@ -100,12 +100,9 @@ sparsed_status make_tensor_map(CUtensorMap* out, const void* base, int batch, in
   return SPARSED_OK;
 }
 
-// One pool of a paged cache: 16-bit [pages, places, heads, 128] with element strides (page, place, head) as [pages, heads, 2
-// halves, places, 64]; box = 64 x 16 places x both halves, 128B swizzle. Cached like the other maps (the sizes that tell two
-// maps apart go into the same key; box_rows = -1 keeps it from meeting theirs).
-sparsed_status make_pool_map(CUtensorMap* out, const void* base, int pages, int places, int heads, int64_t page_stride,
-                             int64_t place_stride, int64_t head_stride) {
-  TensorMapKey key{base, {page_stride, place_stride, head_stride}, pages, heads, places, -1};
+// Any map of 16-bit elements with 128-byte swizzle, cached like those above under a key of its own kind (box_rows < 0).
+sparsed_status make_swizzled_map(CUtensorMap* out, const TensorMapKey& key, int rank, const cuuint64_t* dims,
+                                 const cuuint64_t* stride_bytes, const cuuint32_t* box) {
   TensorMapSlot& slot = g_tensor_maps[tensor_map_slot(key)];
   if (slot.valid && slot.key == key) {
     *out = slot.map;
@@ -113,14 +110,10 @@ sparsed_status make_pool_map(CUtensorMap* out, const void* base, int pages, int 
   }
   EncodeTiledFn enc = encode_tiled_fn();
   if (enc == nullptr) return cuda_fail(cudaErrorNotSupported);
-  cuuint64_t dims[5] = {64, static_cast<cuuint64_t>(places), 2, static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(pages)};
-  cuuint64_t gstrides[4] = {static_cast<cuuint64_t>(place_stride) * 2, 128, static_cast<cuuint64_t>(head_stride) * 2,
-                            static_cast<cuuint64_t>(page_stride) * 2};
-  cuuint32_t box[5] = {64, 16, 2, 1, 1};
-  cuuint32_t elem[5] = {1, 1, 1, 1, 1};
-  CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, gstrides, box, elem,
-                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const cuuint32_t elem[5] = {1, 1, 1, 1, 1};
+  CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, static_cast<cuuint32_t>(rank), const_cast<void*>(key.base), dims,
+                   stride_bytes, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
     g_last_cuda_error = static_cast<int32_t>(r);
     return SPARSED_ERR_CUDA;
@@ -129,6 +122,30 @@ sparsed_status make_pool_map(CUtensorMap* out, const void* base, int pages, int 
   slot.map = *out;
   slot.valid = true;
   return SPARSED_OK;
+}
+
+// One pool of a paged cache, [pages, places, heads, 128] with element strides (page, place, head), as [pages, heads, 2 halves,
+// places, 64]; box = 64 x 16 places x both halves.
+sparsed_status make_pool_map(CUtensorMap* out, const void* base, int pages, int places, int heads, int64_t page_stride,
+                             int64_t place_stride, int64_t head_stride) {
+  const TensorMapKey key{base, {page_stride, place_stride, head_stride}, pages, heads, places, -1};
+  const cuuint64_t dims[5] = {64, static_cast<cuuint64_t>(places), 2, static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(pages)};
+  const cuuint64_t strides[4] = {static_cast<cuuint64_t>(place_stride) * 2, 128, static_cast<cuuint64_t>(head_stride) * 2,
+                                 static_cast<cuuint64_t>(page_stride) * 2};
+  const cuuint32_t box[5] = {64, 16, 2, 1, 1};
+  return make_swizzled_map(out, key, 5, dims, strides, box);
+}
+
+// Packed queries, [total, heads, 128] with element strides (token, head), as [key-value heads, total, heads of a group, 128];
+// box = 64 x `pack` heads x `tokens`.
+sparsed_status make_packed_query_map(CUtensorMap* out, const void* base, int total, int heads_kv, int group, int64_t token_stride,
+                                     int64_t head_stride, int pack, int tokens) {
+  const TensorMapKey key{base, {token_stride, head_stride, group}, heads_kv, pack, total, -2};
+  const cuuint64_t dims[4] = {128, static_cast<cuuint64_t>(group), static_cast<cuuint64_t>(total), static_cast<cuuint64_t>(heads_kv)};
+  const cuuint64_t strides[3] = {static_cast<cuuint64_t>(head_stride) * 2, static_cast<cuuint64_t>(token_stride) * 2,
+                                 static_cast<cuuint64_t>(head_stride) * 2 * group};
+  const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(pack), static_cast<cuuint32_t>(tokens), 1};
+  return make_swizzled_map(out, key, 4, dims, strides, box);
 }
 
 struct Resolved {
@@ -919,8 +936,11 @@ extern "C" sparsed_status sparsed_attn_packed(const sparsed_packed* shape, const
   if ((st = row_strides(shape->k_strides, shape->heads_kv, ks)) != SPARSED_OK) return st;
   if ((st = row_strides(shape->v_strides, shape->heads_kv, vs)) != SPARSED_OK) return st;
   if ((st = row_strides(shape->o_strides, shape->heads_q, os)) != SPARSED_OK) return st;
-  const int64_t tiles = static_cast<int64_t>(shape->total_q) / 128 + shape->num_seqs;
-  if (tiles * shape->heads_q > INT32_MAX) return SPARSED_ERR_UNSUPPORTED;
+  p.group = shape->heads_q / shape->heads_kv;
+  p.pack = packed_heads_per_tile(p.group);
+  p.tile_tokens = 128 / p.pack;
+  const int64_t tiles = static_cast<int64_t>(shape->total_q) / p.tile_tokens + shape->num_seqs;
+  if (tiles * (shape->heads_q / p.pack) > INT32_MAX) return SPARSED_ERR_UNSUPPORTED;
   const bool nothing = shape->num_seqs == 0 || shape->total_q == 0, no_keys = shape->total_k == 0;
   if (cu_q == nullptr || cu_k == nullptr) return SPARSED_ERR_INVALID_ARG;
   if (!nothing && (q == nullptr || o == nullptr)) return SPARSED_ERR_INVALID_ARG;
@@ -932,8 +952,9 @@ extern "C" sparsed_status sparsed_attn_packed(const sparsed_packed* shape, const
   if (nothing) return SPARSED_OK;
   if ((st = check_arch()) != SPARSED_OK) return st;
   CUtensorMap tq, tk, tv;
-  const int64_t q3[3] = {qs[0], qs[1], qs[0]}, k3[3] = {ks[0], ks[1], ks[0]}, v3[3] = {vs[0], vs[1], vs[0]};
-  if ((st = make_tensor_map(&tq, q, 1, shape->heads_q, shape->total_q, q3, 128)) != SPARSED_OK) return st;
+  const int64_t k3[3] = {ks[0], ks[1], ks[0]}, v3[3] = {vs[0], vs[1], vs[0]};
+  if ((st = make_packed_query_map(&tq, q, shape->total_q, shape->heads_kv, p.group, qs[0], qs[1], p.pack, p.tile_tokens)) != SPARSED_OK)
+    return st;
   if (no_keys) {
     tk = tv = tq;   // (nothing is loaded through them)
   } else {
@@ -953,13 +974,12 @@ extern "C" sparsed_status sparsed_attn_packed(const sparsed_packed* shape, const
   p.total_q = shape->total_q;
   p.total_k = shape->total_k;
   p.heads_q = shape->heads_q;
-  p.group = shape->heads_q / shape->heads_kv;
   p.causal = shape->causal;
   p.tiles = static_cast<int>(tiles);
   // key-value heads whose K and V (512 bytes a key) take 48 MB of the L2 together, one at least
   const int64_t heads_in_l2 = (int64_t{48} << 20) / (512ll * (shape->total_k > 0 ? shape->total_k : 1));
-  p.heads_per_pass = static_cast<int>(heads_in_l2 >= shape->heads_kv ? shape->heads_q
-                                                                     : (heads_in_l2 > 1 ? heads_in_l2 : 1) * p.group);
+  const int64_t heads_at_once = heads_in_l2 >= shape->heads_kv ? shape->heads_kv : (heads_in_l2 > 1 ? heads_in_l2 : 1);
+  p.heads_per_pass = static_cast<int>(heads_at_once * (p.group / p.pack));
   p.max_ctas = attn_max_ctas();
   p.slow_path_events = reinterpret_cast<unsigned long long*>(static_cast<uint8_t*>(ws) + 32);
   p.status = static_cast<DeviceStatus*>(ws);

@@ -1,14 +1,21 @@
 // Attention over packed sequences of different lengths, causal or not, head_dim 128, bf16 or fp16, fp32 softmax, on sm_100a.
 //
-// One CTA owns 128 consecutive query rows of one sequence and head and runs the pipeline of attention.cu over the sequence's
-// keys, 64 at a time, up to the last one that its last row sees: a producer warp (TMA into a ring of swizzled tiles), a warp
+// An item is a tile of up to 128 query rows that share their keys: some consecutive tokens of one sequence times some query
+// heads of one key-value head (grouped heads: a tile of 18 tokens x 7 heads is full where 128 tokens of one head are not there,
+// and the diagonal of a causal mask cuts through fewer of its keys). It runs the pipeline of attention.cu over the sequence's
+// keys, 64 at a time, up to the last one that its last token sees: a producer warp (TMA into a ring of swizzled tiles), a warp
 // that issues S_t = Q K_t^T and O += P_t V_t with S, P and O in tensor memory, and four warps with a thread per query row
 // (softmax_pipeline.cuh). Two CTAs per SM.
 //
-// Which rows: the lengths are only known on the device. Sequence b gets the tile numbers from cu_q[b] / 128 + b on: that
-// leaves each sequence room for at least ceil(len / 128) tiles, ascends with b, and needs no sum over the sequences before
-// it, so a CTA finds its sequence with one search in cu_q and the grid, total_q / 128 + num_seqs tiles for each head, is known
-// to the host. Numbers beyond a sequence's last tile are CTAs that leave at once (at most one for each sequence and head).
+// CTAs run from one item into the next, each role by itself: a CTA takes over CTAs of the grid that have not been launched yet
+// (cluster launch control, as the packed walks of attention.cu), and its producer finds the next item's rows and sends its
+// first loads off while the softmax warps are still in the one before. So only a CTA's first item pays for the chain from the
+// offsets over the first loads to the first softmax, and items of different lengths are balanced.
+//
+// Which rows: the lengths are only known on the device. With tiles of T tokens, sequence b gets the tile numbers from
+// cu_q[b] / T + b on: that leaves it room for at least ceil(len / T) tiles, ascends with b, and needs no sum over the sequences
+// before it, so an item's sequence is found by one search in cu_q, and the number of tiles, total_q / T + num_seqs, is known
+// to the host. Numbers beyond a sequence's last tile are empty and passed over (at most one for each sequence).
 //
 // What a row must not see: with a causal mask the logits beyond each row's last key are set to -inf, in the tiles that the
 // diagonal or the sequence's end runs through; all other tiles are walked without a comparison. P is then 0 there, but 0 * V is
@@ -17,8 +24,8 @@
 // finite becomes 0 there, and where it belongs to a key of this sequence, which some rows of the tile see, it is added to
 // those rows' outputs in the epilogue, element by element.
 //
-// Bound: as the dense kernel, the tensor pipe and the softmax warps at the power limit; short sequences by the chain from the
-// offsets to the first softmax.
+// Bound: as the dense kernel, the tensor pipe and the softmax warps at the power limit; short sequences by what an item costs
+// beside its tiles.
 #include "internal.h"
 #include "sequences.cuh"
 #include "softmax_pipeline.cuh"
@@ -35,15 +42,30 @@ constexpr int kColS = 0;      // two S buffers of 64 fp32 columns; P (16-bit pai
 constexpr int kColO = 128;    // O accumulator (fp32, 128 columns)
 constexpr int kSlots = 5;
 
+// What the roles of a CTA need to know of an item.
+struct PackedItem {
+  int num_tiles;     // 64-key tiles to walk; -1: no more items
+  int open_tiles;    // the first of them, all of whose keys all rows see
+  int q_row, tokens; // first row of q and o, and how many tokens the item has
+  int head;          // first query head
+  int first_keys;    // causal: keys that the first token sees (may be negative), one more for each later one
+  int k_row, k_len;  // the sequence's keys
+};
+
 struct PackedSmem {
-  alignas(1024) uint16_t q[2][kTileM * 64];           // two 64-wide halves of head_dim
+  alignas(1024) uint16_t q[2][kTileM * 64];           // two 64-wide halves of head_dim; stages the output too
   alignas(1024) uint16_t kv[kSlots][2][kTileN * 64];
   uint64_t q_full, kv_full[kSlots];
   uint64_t done[kSlots];   // the MMAs that read the slot have completed
   uint64_t p_full[2];
+  uint64_t q_free;         // every softmax warp has read its rows of the output out of the Q buffer: the next Q may land
+  uint64_t item_full[2], item_free[2];   // the producer hands items over through two buffers
+  PackedItem item[2];
+  alignas(16) uint32_t control[4];       // (the launch control's answer)
+  uint64_t control_full;
   uint32_t tmem_base;
   int abort_flag;
-  int special;             // a V of this sequence in a masked tile is infinite or NaN
+  int special[2];          // number of the item in whose masked tiles a V of its sequence is infinite or NaN
 };
 
 // Makes what is not finite in this thread's half row of a 64 x 128 tile of V zero. Returns whether there was any.
@@ -81,96 +103,176 @@ attn_packed_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   const int warp = tid >> 5;
   const int lane = tid & 31;
 
-  // ---- which rows ------------------------------------------------------------------------
-  // Heads are taken heads_per_pass at a time (their K and V stay in L2), tiles from the last one down: with a causal mask a
-  // sequence's last tiles are its longest.
-  const int per_pass = p.tiles * p.heads_per_pass;
-  const int pass = blockIdx.x / per_pass;
-  const int heads_here = min(p.heads_per_pass, p.heads_q - pass * p.heads_per_pass);
-  const int in_pass = blockIdx.x - pass * per_pass;
-  const int tile = p.tiles - 1 - in_pass / heads_here;
-  const int head = pass * p.heads_per_pass + in_pass % heads_here;
-  const int kv_head = head / p.group;
-  const int seq = last_not_above(p.num_seqs, tile, [&](int b) { return __ldcg(p.cu_q + b) / kTileM + b; });
-  const int2 q_rows = sequence_rows(p.cu_q, seq, p.total_q, p.status, 4);
-  const int2 k_rows = sequence_rows(p.cu_k, seq, p.total_k, p.status, 5);
-  const int q_len = q_rows.y - q_rows.x, k_len = k_rows.y - k_rows.x;
-  const int q0 = (tile - (q_rows.x / kTileM + seq)) * kTileM;   // the CTA's first row in its sequence
-  if (q0 < 0 || q0 >= q_len) return;
-  const int shift = k_len - q_len;   // causal: row i sees keys up to i + shift
-  const int seen = p.causal ? min(max(min(q0 + kTileM, q_len) + shift, 0), k_len) : k_len;   // keys the CTA walks
-  const int num_tiles = (seen + kTileN - 1) / kTileN;
-  // keys that all its rows see, in tiles: these need no mask
-  const int open_tiles = (p.causal ? min(max(q0 + 1 + shift, 0), k_len) : k_len) / kTileN;
-
-  if (num_tiles == 0) {
-    // no keys: zeros, and a log-sum-exp of -inf
-    for (int i = tid; i < kTileM * 16; i += kThreads) {
-      const int row = q0 + (i >> 4);
-      if (row < q_len)
-        reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + (q_rows.x + row) * p.o_stride_t + head * p.o_stride_h)[i & 15] =
-            make_uint4(0u, 0u, 0u, 0u);
-    }
-    if (p.lse != nullptr && tid < kTileM && q0 + tid < q_len)
-      p.lse[static_cast<int64_t>(head) * p.total_q + q_rows.x + q0 + tid] = -INFINITY;
-    return;
-  }
-
-  // ---- set-up: the producer warp starts its first loads before the CTA-wide part has finished ---------------
-  auto issue_load = [&](int slot, int which, int t) {
-    if (elect_one_sync()) {
-      const CUtensorMap* tm = which == 0 ? &tm_k : &tm_v;
-      mbar_expect_tx(&sm.kv_full[slot], kTileN * kHeadDim * 2);   // (rows beyond the tensor arrive as zeros)
-      tma_load_4d(sm.kv[slot][0], tm, &sm.kv_full[slot], 0, k_rows.x + t * kTileN, kv_head, 0);
-      tma_load_4d(sm.kv[slot][1], tm, &sm.kv_full[slot], 64, k_rows.x + t * kTileN, kv_head, 0);
-    }
-    __syncwarp();
-  };
-  const int early = min(2 * num_tiles, kSlots);
-  if (warp == 4) {
-    if (lane == 0) {
-      mbar_init(&sm.q_full, 1);
-      for (int s = 0; s < kSlots; ++s) mbar_init(&sm.kv_full[s], 1);
-      mbar_fence_init();
-    }
-    __syncwarp();
-    if (elect_one_sync()) {
-      tma_prefetch_desc(&tm_q);
-      tma_prefetch_desc(&tm_k);
-      tma_prefetch_desc(&tm_v);
-      mbar_expect_tx(&sm.q_full, kTileM * kHeadDim * 2);
-      tma_load_4d(sm.q[0], &tm_q, &sm.q_full, 0, q_rows.x + q0, head, 0);
-      tma_load_4d(sm.q[1], &tm_q, &sm.q_full, 64, q_rows.x + q0, head, 0);
-    }
-    __syncwarp();
-    for (int i = 0; i < early; ++i) issue_load(i, i & 1, i >> 1);
-  }
+  // ---- set-up --------------------------------------------------------------------------
   if (tid == 0) {
-    for (int s = 0; s < kSlots; ++s) mbar_init(&sm.done[s], 1);
-    for (int s = 0; s < 2; ++s) mbar_init(&sm.p_full[s], kSoftmaxThreads);
+    mbar_init(&sm.q_full, 1);
+    mbar_init(&sm.q_free, 4);
+    for (int s = 0; s < kSlots; ++s) {
+      mbar_init(&sm.kv_full[s], 1);
+      mbar_init(&sm.done[s], 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&sm.p_full[s], kSoftmaxThreads);
+      mbar_init(&sm.item_full[s], 1);
+      mbar_init(&sm.item_free[s], 5);   // four softmax warps and the issuer
+      sm.special[s] = -1;
+    }
+    mbar_init(&sm.control_full, 1);
     sm.abort_flag = 0;
-    sm.special = 0;
     mbar_fence_init();
   }
   if (warp == 5) {
     tmem_alloc(&sm.tmem_base, kTmemCols);
     tmem_relinquish();
   }
+  if (warp == 4 && elect_one_sync()) {
+    tma_prefetch_desc(&tm_q);
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sm.tmem_base;
   const uint32_t tO = tmem + kColO;
-  int loads_issued = early;
 
+  // Warps 4 and 5 run their loops with all 32 lanes converged and let one elected lane issue.
   if (warp == 4) {
-    // =============================== TMA producer =======================================
-    for (int i = early; i < 2 * num_tiles; ++i) {
-      const int slot = i % kSlots;
-      bool ok = mbar_wait(&sm.done[slot], ((i / kSlots) - 1) & 1, &sm.abort_flag, p.status, 110);
-      if (!__all_sync(0xffffffffu, ok)) break;
-      issue_load(slot, i & 1, i >> 1);
-      loads_issued = i + 1;
+    // =============================== producer ===========================================
+    // Heads are taken heads_per_pass at a time (their K and V stay in L2), tiles from the last one down: with a causal mask a
+    // sequence's last tiles are its longest.
+    const int packed_heads = p.heads_q / p.pack, per_pass = p.tiles * p.heads_per_pass;
+    PackedItem it;
+    // what grid number `number` is; false: an empty tile
+    auto describe = [&](int number) -> bool {
+      const int pass = number / per_pass, in_pass = number - pass * per_pass;
+      const int heads_here = min(p.heads_per_pass, packed_heads - pass * p.heads_per_pass);
+      const int tile = p.tiles - 1 - in_pass / heads_here;
+      it.head = (pass * p.heads_per_pass + in_pass % heads_here) * p.pack;
+      const int seq = last_not_above(p.num_seqs, tile, [&](int b) { return __ldcg(p.cu_q + b) / p.tile_tokens + b; });
+      const int2 q_rows = sequence_rows(p.cu_q, seq, p.total_q, p.status, 4);
+      const int2 k_rows = sequence_rows(p.cu_k, seq, p.total_k, p.status, 5);
+      const int q_len = q_rows.y - q_rows.x;
+      const int q0 = (tile - (q_rows.x / p.tile_tokens + seq)) * p.tile_tokens;   // the tile's first token in its sequence
+      if (q0 < 0 || q0 >= q_len) return false;
+      it.q_row = q_rows.x + q0;
+      it.tokens = min(p.tile_tokens, q_len - q0);
+      it.k_row = k_rows.x;
+      it.k_len = k_rows.y - k_rows.x;
+      it.first_keys = p.causal ? q0 + 1 + it.k_len - q_len : it.k_len;
+      const int seen = p.causal ? min(max(it.first_keys + it.tokens - 1, 0), it.k_len) : it.k_len;
+      it.num_tiles = (seen + kTileN - 1) / kTileN;
+      it.open_tiles = min(max(it.first_keys, 0), it.k_len) / kTileN;
+      return true;
+    };
+    auto request_item = [&]() {
+      if (elect_one_sync()) {
+        mbar_expect_tx(&sm.control_full, 16);
+        launch_control_request(sm.control, &sm.control_full);
+      }
+      __syncwarp();
+    };
+    auto publish = [&](int buf) {
+      __syncwarp();
+      if (lane == 0) {
+        sm.item[buf] = it;
+        mbar_arrive(&sm.item_full[buf]);
+      }
+      __syncwarp();
+    };
+    bool ok = true, asked = false;
+    uint32_t requests = 0, answers = 0;   // of the launch control
+    int load0 = 0, q_tiles = 0;           // K / V loads and Q tiles of earlier items
+    int issued = 0, q_issued = 0;
+    int number = blockIdx.x;
+    for (int nth = 0; ok; ++nth) {        // the CTA's nth item, in item buffer nth & 1
+      bool found = nth == 0 && describe(number);
+      while (!found) {
+        if (!asked) {
+          request_item();
+          ++requests;
+        }
+        asked = false;
+        ok = mbar_wait(&sm.control_full, answers & 1, &sm.abort_flag, p.status, 113);
+        if (!(ok = __all_sync(0xffffffffu, ok))) break;
+        ++answers;
+        number = launch_control_answer(sm.control);
+        __syncwarp();
+        if (number < 0) break;
+        found = describe(number);
+      }
+      // the other roles have finished with the item that was in this buffer
+      if (ok && nth >= 2) {
+        ok = mbar_wait(&sm.item_free[nth & 1], ((nth >> 1) - 1) & 1, &sm.abort_flag, p.status, 112);
+        ok = __all_sync(0xffffffffu, ok);
+      }
+      if (!ok) break;
+      if (!found) {
+        it.num_tiles = -1;
+        publish(nth & 1);
+        break;
+      }
+      publish(nth & 1);
+      const int loads = 2 * it.num_tiles;
+      // The Q buffer doubles as the staging tile of the output before: the next Q may land once that has been read out. The
+      // first ring-full of the item's K / V loads does not depend on it and goes out first.
+      bool q_pending = loads > 0;
+      auto settle_q = [&]() -> bool {
+        bool got = true;
+        if (q_tiles > 0) {
+          got = mbar_wait(&sm.q_free, (q_tiles - 1) & 1, &sm.abort_flag, p.status, 111);
+          got = __all_sync(0xffffffffu, got);
+        }
+        if (got && elect_one_sync()) {
+          mbar_expect_tx(&sm.q_full, p.tile_tokens * p.pack * kHeadDim * 2);   // rows beyond the tensor arrive as zeros
+          const int group = it.head / p.group, first = it.head - group * p.group;
+          tma_load_4d(sm.q[0], &tm_q, &sm.q_full, 0, first, it.q_row, group);
+          tma_load_4d(sm.q[1], &tm_q, &sm.q_full, 64, first, it.q_row, group);
+        }
+        __syncwarp();
+        if (got) ++q_issued;
+        q_pending = false;
+        return got;
+      };
+      const int kv_head = it.head / p.group;
+      const int q_at = nth == 0 ? 0 : min(loads, kSlots);
+      // The next item is asked for two tiles before this one's last load: late enough that a CTA with a long item does not hold
+      // one that another could have started, early enough for the answer to be there.
+      const int request_at = max(loads - 4, 0);
+      for (int i = 0; i < loads; ++i) {
+        if (q_pending && i == q_at && !(ok = settle_q())) break;
+        if (i == request_at) {
+          request_item();
+          ++requests;
+          asked = true;
+        }
+        const int g = load0 + i, slot = g % kSlots;
+        if (g >= kSlots) {
+          ok = mbar_wait(&sm.done[slot], ((g / kSlots) - 1) & 1, &sm.abort_flag, p.status, 110);
+          if (!(ok = __all_sync(0xffffffffu, ok))) break;
+        }
+        if (elect_one_sync()) {
+          const CUtensorMap* tm = (i & 1) == 0 ? &tm_k : &tm_v;
+          mbar_expect_tx(&sm.kv_full[slot], kTileN * kHeadDim * 2);
+          tma_load_4d(sm.kv[slot][0], tm, &sm.kv_full[slot], 0, it.k_row + (i >> 1) * kTileN, kv_head, 0);
+          tma_load_4d(sm.kv[slot][1], tm, &sm.kv_full[slot], 64, it.k_row + (i >> 1) * kTileN, kv_head, 0);
+        }
+        __syncwarp();
+        issued = g + 1;
+      }
+      if (ok && q_pending) ok = settle_q();
+      load0 += loads;
+      if (loads > 0) ++q_tiles;
+    }
+    if (!ok) {
+      // given up: what is on its way must land before the CTA leaves (bounded like every wait)
+      auto drain = [&](uint64_t* bar, uint32_t phase) {
+        for (uint32_t n = 0; n < kSpinLimit && !mbar_try_wait(bar, phase); ++n) {
+        }
+      };
+      if (requests > answers) drain(&sm.control_full, answers & 1);
+      for (int g = max(issued - kSlots, 0); g < issued; ++g) drain(&sm.kv_full[g % kSlots], (g / kSlots) & 1);
+      if (q_issued > 0) drain(&sm.q_full, (q_issued - 1) & 1);
     }
   } else if (warp == 5) {
     // =============================== UMMA issuer ========================================
@@ -178,120 +280,171 @@ attn_packed_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     const uint32_t kv_lo0 = umma_desc_lo(smem_u32(sm.kv[0][0]), 16);            // as K (K-major)
     const uint32_t v_lo0 = umma_desc_lo(smem_u32(sm.kv[0][0]), kTileN * 128);   // as V (MN-major)
     constexpr uint32_t slot_step = (2 * kTileN * 64 * 2) >> 4;                  // 16 KB per ring slot
-    auto issue_qk = [&](int t) -> bool {
-      const int slot = (2 * t) % kSlots;
-      bool got = mbar_wait(&sm.kv_full[slot], ((2 * t) / kSlots) & 1, &sm.abort_flag, p.status, 121);
-      got = __all_sync(0xffffffffu, got);
-      if (!got) return false;
-      issue_qk64<Type>(tmem + kColS + (t & 1) * kTileN, q_lo0, kv_lo0 + slot * slot_step, &sm.done[slot]);
-      return true;
-    };
-    bool ok = mbar_wait(&sm.q_full, 0, &sm.abort_flag, p.status, 120);
-    ok = __all_sync(0xffffffffu, ok);
-    ok = ok && issue_qk(0);
-    for (int t = 0; ok && t < num_tiles; ++t) {
-      if (t + 1 < num_tiles && !issue_qk(t + 1)) break;
-      const int g = 2 * t + 1;
-      const int slot = g % kSlots;
-      ok = mbar_wait2(&sm.p_full[t & 1], (t >> 1) & 1, &sm.kv_full[slot], (g / kSlots) & 1, &sm.abort_flag, p.status, 122);
+    bool ok = true;
+    int load0 = 0, tile0 = 0, q_tiles = 0;   // loads / tiles / Q tiles of earlier items
+    for (int nth = 0; ok; ++nth) {
+      const int buf = nth & 1;
+      ok = mbar_wait(&sm.item_full[buf], (nth >> 1) & 1, &sm.abort_flag, p.status, 123);
+      if (!(ok = __all_sync(0xffffffffu, ok))) break;
+      const int num_tiles = sm.item[buf].num_tiles;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.item_free[buf]);
+      if (num_tiles < 0) break;
+      if (num_tiles == 0) continue;
+      auto issue_qk = [&](int t) -> bool {
+        const int g = load0 + 2 * t, slot = g % kSlots;
+        bool got = mbar_wait(&sm.kv_full[slot], (g / kSlots) & 1, &sm.abort_flag, p.status, 121);
+        got = __all_sync(0xffffffffu, got);
+        if (!got) return false;
+        issue_qk64<Type>(tmem + kColS + ((tile0 + t) & 1) * kTileN, q_lo0, kv_lo0 + slot * slot_step, &sm.done[slot]);
+        return true;
+      };
+      ok = mbar_wait(&sm.q_full, q_tiles & 1, &sm.abort_flag, p.status, 120);
       ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      issue_pv64<Type>(tO, tmem + kColS + (t & 1) * kTileN, v_lo0 + slot * slot_step, t > 0, &sm.done[slot]);
+      ++q_tiles;
+      ok = ok && issue_qk(0);
+      for (int t = 0; ok && t < num_tiles; ++t) {
+        // The S buffer of tile t+1 last held P of the tile two before it, whose P V was issued
+        // earlier by this thread, and tcgen05 operations of one thread execute in issue order.
+        if (t + 1 < num_tiles && !(ok = issue_qk(t + 1))) break;
+        const int g = load0 + 2 * t + 1, slot = g % kSlots, gt = tile0 + t;
+        ok = mbar_wait2(&sm.p_full[gt & 1], (gt >> 1) & 1, &sm.kv_full[slot], (g / kSlots) & 1, &sm.abort_flag, p.status, 122);
+        if (!(ok = __all_sync(0xffffffffu, ok))) break;
+        // the first P V of an item overwrites O: the softmax warps handed P over after they had read the previous item's O
+        issue_pv64<Type>(tO, tmem + kColS + (gt & 1) * kTileN, v_lo0 + slot * slot_step, t > 0, &sm.done[slot]);
+      }
+      load0 += 2 * num_tiles;
+      tile0 += num_tiles;
     }
   } else {
     // =============================== softmax / epilogue =================================
     const uint32_t lane_base = static_cast<uint32_t>(warp * 32) << 16;
     const float scale_log2 = p.scale_log2;
-    const int row = q0 + tid;                 // in the sequence
-    const bool row_valid = row < q_len;       // rows behind the sequence's end belong to others; nothing of them is kept
-    const int row_keys = p.causal ? min(max(row + 1 + shift, 0), k_len) : k_len;   // keys the row sees
-    // tiles that all rows of this warp see entirely (lane 0's row sees the fewest keys)
-    const int warp_open = __shfl_sync(0xffffffffu, row_keys, 0) / kTileN;
-    RowState st{-INFINITY, 0.f};
+    // this thread's row of every item: token tid / pack, head tid % pack (worked out where needed, to save registers)
+    auto token = [&]() -> int { return tid / p.pack; };
     bool ok = true;
-    for (int t = 0; t < num_tiles; ++t) {
-      const int gk = 2 * t;
-      ok = mbar_wait(&sm.done[gk % kSlots], (gk / kSlots) & 1, &sm.abort_flag, p.status, 130);
+    int load0 = 0, tile0 = 0;   // loads / tiles of earlier items
+    for (int nth = 0; ok; ++nth) {
+      ok = mbar_wait(&sm.item_full[nth & 1], (nth >> 1) & 1, &sm.abort_flag, p.status, 133);
       if (!(ok = __all_sync(0xffffffffu, ok))) break;
-      tc_fence_after();
-      const uint32_t tS = tmem + kColS + (t & 1) * kTileN + lane_base;
-      uint32_t r0[32], r1[32], pk[32];
-      tmem_ld32(tS, r0);
-      tmem_ld32(tS + 32, r1);
-      tmem_wait_ld();
-      if (t >= warp_open) mask_columns_from(r0, r1, row_keys - t * kTileN);
-      float2 sums = make_float2(0.f, 0.f);
-      bool exact = row_valid && st.m == -INFINITY;   // nothing accumulated yet: no reference maximum to try
-      if (!__any_sync(0xffffffffu, exact)) {
-        sums = softmax_group_fast<Type>(r0, r1, scale_log2, st.m, pk);
-        exact = row_valid && !(sums.x + sums.y <= 256.0f);   // logits outgrew the running maximum (or NaN)
+      // (read again where it is needed: few registers are left beside a row of S)
+      const PackedItem& it = sm.item[nth & 1];
+      const int num_tiles = it.num_tiles, open_tiles = it.open_tiles;
+      if (num_tiles < 0) break;
+      // (rows behind the item's end are nobody's)
+      auto row_valid = [&]() -> bool { return token() < min(it.tokens, p.tile_tokens); };
+      auto out_at = [&]() -> int64_t {
+        const int tok = token();
+        return static_cast<int64_t>(it.q_row + tok) * p.o_stride_t + (it.head + tid - tok * p.pack) * p.o_stride_h;
+      };
+      auto store_lse = [&](float lse) {
+        const int tok = token();
+        p.lse[static_cast<int64_t>(it.head + tid - tok * p.pack) * p.total_q + it.q_row + tok] = lse;
+      };
+      auto release_item = [&]() {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.item_free[nth & 1]);
+      };
+      if (num_tiles == 0) {
+        // no keys: zeros, and a log-sum-exp of -inf
+        if (row_valid()) {
+          uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + out_at());
+          for (int i = 0; i < 16; ++i) o[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (p.lse != nullptr) store_lse(-INFINITY);
+        }
+        release_item();
+        continue;
       }
-      if (__any_sync(0xffffffffu, exact)) {
-        // Rows whose reference has to move take their own maximum of the tile; the others keep theirs and get the same P
-        // again, so that a row's result does not depend on its neighbours (later tokens, with a causal mask).
-        float alpha = 1.f;
-        if (exact) {
-          float top = -INFINITY;
+      // keys this row sees
+      auto keys_of_row = [&]() -> int { return p.causal ? min(max(it.first_keys + token(), 0), it.k_len) : it.k_len; };
+      // (a row that is nobody's holds anything: a finite reference keeps it from asking for the exact path in every tile)
+      RowState st{row_valid() ? -INFINITY : 0.f, 0.f};
+      for (int t = 0; t < num_tiles; ++t) {
+        const int gk = load0 + 2 * t;
+        ok = mbar_wait(&sm.done[gk % kSlots], (gk / kSlots) & 1, &sm.abort_flag, p.status, 130);
+        if (!(ok = __all_sync(0xffffffffu, ok))) break;
+        tc_fence_after();
+        const int buf = (tile0 + t) & 1;
+        const uint32_t tS = tmem + kColS + buf * kTileN + lane_base;
+        uint32_t r0[32], r1[32], pk[32];
+        tmem_ld32(tS, r0);
+        tmem_ld32(tS + 32, r1);
+        tmem_wait_ld();
+        if (t >= open_tiles) mask_columns_from(r0, r1, keys_of_row() - t * kTileN);
+        float2 sums = make_float2(0.f, 0.f);
+        bool exact = st.m == -INFINITY;   // nothing accumulated yet: no reference maximum to try
+        if (!__any_sync(0xffffffffu, exact)) {
+          sums = softmax_group_fast<Type>(r0, r1, scale_log2, st.m, pk);
+          exact = sums.x + sums.y > 256.0f;   // logits outgrew the running maximum (a NaN makes the row NaN either way)
+        }
+        if (__any_sync(0xffffffffu, exact)) {
+          // Rows whose reference has to move take their own maximum of the tile; the others keep theirs and get the same P
+          // again, so that a row's result does not depend on its neighbours (later tokens, with a causal mask).
+          float alpha = 1.f;
+          if (exact) {
+            float top = -INFINITY;
 #pragma unroll
-          for (int j = 0; j < 32; ++j) top = fmaxf(top, fmaxf(__uint_as_float(r0[j]), __uint_as_float(r1[j])));
-          top *= scale_log2;
-          if (top > st.m) {
-            alpha = fast_exp2(st.m - top);   // 0 when nothing was accumulated yet
-            st.m = top;
-            st.l *= alpha;
+            for (int j = 0; j < 32; ++j) top = fmaxf(top, fmaxf(__uint_as_float(r0[j]), __uint_as_float(r1[j])));
+            top *= scale_log2;
+            if (top > st.m) {
+              alpha = fast_exp2(st.m - top);   // 0 when nothing was accumulated yet
+              st.m = top;
+              st.l *= alpha;
+            }
+          }
+          // (a row whose logits so far are all -inf: 2^(-inf - 0) = 0, not NaN)
+          sums = softmax_group_fast<Type>(r0, r1, scale_log2, st.m == -INFINITY ? 0.f : st.m, pk);
+          if (t > 0) {
+            // O must be quiescent: wait until P_{t-1} V_{t-1} (which read ring load 2t-1) has drained
+            const int gp = load0 + 2 * t - 1;
+            ok = mbar_wait(&sm.done[gp % kSlots], (gp / kSlots) & 1, &sm.abort_flag, p.status, 132);
+            if (!(ok = __all_sync(0xffffffffu, ok))) break;
+            tc_fence_after();
+            rescale_accumulator_row(tO + lane_base, alpha);
+            if (lane == 0) atomicAdd(p.slow_path_events, 1ull);
           }
         }
-        // (a row whose logits so far are all -inf: 2^(-inf - 0) = 0, not NaN)
-        sums = softmax_group_fast<Type>(r0, r1, scale_log2, st.m == -INFINITY ? 0.f : st.m, pk);
-        if (t > 0) {
-          // O must be quiescent: wait until P_{t-1} V_{t-1} (which read ring load 2t-1) has drained
-          const int gp = 2 * t - 1;
-          ok = mbar_wait(&sm.done[gp % kSlots], (gp / kSlots) & 1, &sm.abort_flag, p.status, 132);
+        st.l += sums.x + sums.y;
+        tmem_st32(tS, pk);  // P_t over the first 32 columns of S_t
+        tmem_wait_st();
+        if (t >= open_tiles) {
+          // some row of the item does not see all of these keys
+          const int g = load0 + 2 * t + 1;
+          ok = mbar_wait(&sm.kv_full[g % kSlots], (g / kSlots) & 1, &sm.abort_flag, p.status, 134);
           if (!(ok = __all_sync(0xffffffffu, ok))) break;
-          tc_fence_after();
-          rescale_accumulator_row(tO + lane_base, alpha);
-          if (lane == 0) atomicAdd(p.slow_path_events, 1ull);
+          const int key = tid & 63;
+          if (clean_half_row<Type>(sm.kv[g % kSlots][tid >> 6], key)) {
+            if (t * kTileN + key < it.k_len) sm.special[nth & 1] = nth;
+            fence_proxy_async_smem();
+          }
         }
+        tc_fence_before();
+        mbar_arrive(&sm.p_full[buf]);
       }
-      st.l += sums.x + sums.y;
-      tmem_st32(tS, pk);  // P_t over the first 32 columns of S_t
-      tmem_wait_st();
-      if (t >= open_tiles) {
-        // some row of the CTA does not see all of this tile's keys
-        const int g = 2 * t + 1;
-        ok = mbar_wait(&sm.kv_full[g % kSlots], (g / kSlots) & 1, &sm.abort_flag, p.status, 133);
-        if (!(ok = __all_sync(0xffffffffu, ok))) break;
-        const int key = tid & 63;
-        if (clean_half_row<Type>(sm.kv[g % kSlots][tid >> 6], key)) {
-          if (t * kTileN + key < k_len) sm.special = 1;
-          fence_proxy_async_smem();
-        }
+      // ---- epilogue: O / l -> 16 bits -> shared memory (the dead Q tile) -> global, each warp its own rows --------
+      if (ok) {
+        const int gl = load0 + 2 * num_tiles - 1;   // the last P V read this load's slot
+        ok = mbar_wait(&sm.done[gl % kSlots], (gl / kSlots) & 1, &sm.abort_flag, p.status, 131);
       }
-      tc_fence_before();
-      mbar_arrive(&sm.p_full[t & 1]);
-    }
-    // ---- epilogue: O / l -> 16 bits -> shared memory (the dead Q tile) -> global, each warp its own rows --------
-    if (ok) {
-      const int gl = 2 * (num_tiles - 1) + 1;   // the last P V read this load's slot
-      ok = mbar_wait(&sm.done[gl % kSlots], (gl / kSlots) & 1, &sm.abort_flag, p.status, 131);
-    }
-    named_barrier_sync(1, kSoftmaxThreads);     // (all threads reach it; `special` is settled)
-    if (*reinterpret_cast<volatile int*>(&sm.abort_flag) == 0) {
+      if (!(ok = __all_sync(0xffffffffu, ok))) break;
       tc_fence_after();
       // a row of no keys has accumulated P = 0: zeros
       const float inv_l = st.l > 0.f ? (1.f / st.l) : (st.l == 0.f ? 0.f : st.l);
       stage_output_half<Type>(tO + lane_base, true, inv_l, reinterpret_cast<__nv_bfloat16*>(sm.q[0]), tid);
       stage_output_half<Type>(tO + lane_base + 64, true, inv_l, reinterpret_cast<__nv_bfloat16*>(sm.q[1]), tid);
-      if (*reinterpret_cast<volatile int*>(&sm.special) != 0 && row_valid) {
+      tc_fence_before();   // the next item's first P V overwrites O: order these reads before its hand-over
+      // (all threads wrote their notes before the hand-over of the P whose P V has just been waited for)
+      if (*reinterpret_cast<volatile int*>(&sm.special[nth & 1]) == nth && row_valid()) {
         // what was taken out of V in the masked tiles: a probability times an infinity or NaN is that infinity or NaN
+        const int kv_head = it.head / p.group, row_keys = keys_of_row();
         for (int d = 0; d < kHeadDim; d += 2) {
           uint32_t* at = reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(sm.q[d >> 6]) + tid * 128 +
                                                      ((((d & 63) >> 3) ^ (tid & 7)) << 4) + (d & 7) * 2);
           float2 sum = Type::unpack(*at);
           bool any = false;
-          for (int j = open_tiles * kTileN; j < row_keys; ++j) {
+          for (int j = it.open_tiles * kTileN; j < row_keys; ++j) {
             const uint32_t x = __ldcg(reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p.v) +
-                                                                        (k_rows.x + j) * p.v_stride_t + kv_head * p.v_stride_h + d));
+                                                                        (it.k_row + j) * p.v_stride_t + kv_head * p.v_stride_h + d));
             const uint32_t bad = non_finite_pair<Type>(x);
             const float2 f = Type::unpack(x);
             if (bad & 0x8000u) sum.x += f.x;
@@ -303,32 +456,29 @@ attn_packed_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       }
       __syncwarp();
       // sixteen threads to a row's 256 bytes
-      uint16_t* o = static_cast<uint16_t*>(p.o) + (q_rows.x + static_cast<int64_t>(q0)) * p.o_stride_t + head * p.o_stride_h;
+      const int64_t out = out_at();
+      const bool stored = row_valid();
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int r = warp * 32 + 2 * i + (lane >> 4);
-        const int chunk = lane & 7;
+        const int from = 2 * i + (lane >> 4), r = warp * 32 + from;
         const uint4 x = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(sm.q[(lane >> 3) & 1]) + r * 128 +
-                                                        ((chunk ^ (r & 7)) << 4));
-        if (q0 + r < q_len) *reinterpret_cast<uint4*>(o + r * p.o_stride_t + (lane & 15) * 8) = x;
+                                                        (((lane & 7) ^ (r & 7)) << 4));
+        const int64_t to = __shfl_sync(0xffffffffu, out, from);
+        if (__shfl_sync(0xffffffffu, stored, from)) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + to + (lane & 15) * 8) = x;
       }
-      if (p.lse != nullptr && row_valid)
-        p.lse[static_cast<int64_t>(head) * p.total_q + q_rows.x + row] = (st.m + log2f(st.l)) * 0.69314718055994531f;
+      fence_proxy_async_smem();   // (the next Q comes through the async proxy)
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.q_free);
+      if (p.lse != nullptr && stored) store_lse((st.m + log2f(st.l)) * 0.69314718055994531f);
+      release_item();
+      load0 += 2 * num_tiles;
+      tile0 += num_tiles;
     }
   }
 
   // ---- teardown ------------------------------------------------------------------------
   tc_fence_before();
   __syncthreads();
-  if (warp == 4 && sm.abort_flag != 0) {
-    // given up: the loads in flight must have landed before the CTA leaves (bounded like every wait)
-    auto drain = [&](uint64_t* bar, uint32_t phase) {
-      for (uint32_t n = 0; n < kSpinLimit && !mbar_try_wait(bar, phase); ++n) {
-      }
-    };
-    for (int i = max(loads_issued - kSlots, 0); i < loads_issued; ++i) drain(&sm.kv_full[i % kSlots], (i / kSlots) & 1);
-    drain(&sm.q_full, 0);
-  }
   if (warp == 5) {
     __syncwarp();
     tmem_dealloc(tmem, kTmemCols);
@@ -344,10 +494,17 @@ cudaError_t launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorM
   static SmemLimit limit;  // per template instantiation
   cudaError_t e = ensure_dynamic_smem(kernel, smem, limit);
   if (e != cudaSuccess) return e;
-  return launch_overlapped(kernel, static_cast<long long>(p.tiles) * p.heads_q, p.max_ctas, kThreads, smem, stream, tq, tk, tv, p);
+  return launch_overlapped(kernel, static_cast<long long>(p.tiles) * (p.heads_q / p.pack), p.max_ctas, kThreads, smem, stream, tq, tk, tv, p);
 }
 
 }  // namespace
+
+int packed_heads_per_tile(int group) {
+  int pack = 1;
+  for (int d = 2; d <= group && d <= kTileM; ++d)
+    if (group % d == 0 && kTileM / d * d >= 124) pack = d;
+  return pack;
+}
 
 cudaError_t launch_attn_packed(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const PackedParams& p,
                                bool fp16, cudaStream_t stream) {

@@ -16,15 +16,20 @@ struct PackedParams {
   int num_seqs, total_q, total_k, heads_q;
   int group;               // heads_q / heads_kv
   int causal;
-  int tiles;               // total_q / 128 + num_seqs: numbers of query tiles, some of them empty (attention_packed.cu)
-  int heads_per_pass;      // query heads whose tiles are taken before those of the next ones
+  int pack;                // query heads of a group that share a tile (packed_heads_per_tile)
+  int tile_tokens;         // 128 / pack
+  int tiles;               // total_q / tile_tokens + num_seqs: numbers of query tiles, some of them empty
+  int heads_per_pass;      // tiles' worth of heads that are taken before the next ones
   int max_ctas;            // CTAs that fit on the device at once (0: not known)
   float scale_log2;
   unsigned long long* slow_path_events;
   DeviceStatus* status;
 };
 
-// (Q's tensor map: [heads, total, 128] as batch 1, boxes of 64 x 128 rows; K and V: 64 x 64)
+// Query heads of a group that share a tile of 128 rows: the most that divide the group and leave at most 4 rows unused.
+int packed_heads_per_tile(int group);
+// (Q's tensor map: [heads_kv, total, group, 128], boxes of 64 x pack x tile_tokens; K's and V's as in attention.cu, boxes of
+// 64 x 64 rows)
 cudaError_t launch_attn_packed(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const PackedParams& p,
                                bool fp16, cudaStream_t stream);
 
