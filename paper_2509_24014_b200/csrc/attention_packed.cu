@@ -88,6 +88,13 @@ __device__ __forceinline__ bool clean_half_row(uint16_t* half_tile, int row) {
   return true;
 }
 
+// -inf in the columns at and beyond `valid` of 32
+__device__ __forceinline__ void mask_half(uint32_t (&r)[32], int valid) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j)
+    if (j >= valid) r[j] = 0xff800000u;
+}
+
 template <class Type>
 __global__ void __launch_bounds__(kThreads, 2)
 attn_packed_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
@@ -320,8 +327,7 @@ attn_packed_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     // =============================== softmax / epilogue =================================
     const uint32_t lane_base = static_cast<uint32_t>(warp * 32) << 16;
     const float scale_log2 = p.scale_log2;
-    // this thread's row of every item: token tid / pack, head tid % pack (worked out where needed, to save registers)
-    auto token = [&]() -> int { return tid / p.pack; };
+    const int token = tid / p.pack;   // this thread's row of every item: this token, head tid % pack
     bool ok = true;
     int load0 = 0, tile0 = 0;   // loads / tiles of earlier items
     for (int nth = 0; ok; ++nth) {
@@ -332,14 +338,12 @@ attn_packed_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       const int num_tiles = it.num_tiles, open_tiles = it.open_tiles;
       if (num_tiles < 0) break;
       // (rows behind the item's end are nobody's)
-      auto row_valid = [&]() -> bool { return token() < min(it.tokens, p.tile_tokens); };
+      auto row_valid = [&]() -> bool { return token < min(it.tokens, p.tile_tokens); };
       auto out_at = [&]() -> int64_t {
-        const int tok = token();
-        return static_cast<int64_t>(it.q_row + tok) * p.o_stride_t + (it.head + tid - tok * p.pack) * p.o_stride_h;
+        return static_cast<int64_t>(it.q_row + token) * p.o_stride_t + (it.head + tid - token * p.pack) * p.o_stride_h;
       };
       auto store_lse = [&](float lse) {
-        const int tok = token();
-        p.lse[static_cast<int64_t>(it.head + tid - tok * p.pack) * p.total_q + it.q_row + tok] = lse;
+        p.lse[static_cast<int64_t>(it.head + tid - token * p.pack) * p.total_q + it.q_row + token] = lse;
       };
       auto release_item = [&]() {
         __syncwarp();
@@ -356,10 +360,21 @@ attn_packed_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         continue;
       }
       // keys this row sees
-      auto keys_of_row = [&]() -> int { return p.causal ? min(max(it.first_keys + token(), 0), it.k_len) : it.k_len; };
+      auto keys_of_row = [&]() -> int { return p.causal ? min(max(it.first_keys + token, 0), it.k_len) : it.k_len; };
       // (a row that is nobody's holds anything: a finite reference keeps it from asking for the exact path in every tile)
       RowState st{row_valid() ? -INFINITY : 0.f, 0.f};
       for (int t = 0; t < num_tiles; ++t) {
+        if (t >= open_tiles) {
+          // Some row of the item does not see all of these keys: V is looked at while S_t is still being worked out.
+          const int g = load0 + 2 * t + 1;
+          ok = mbar_wait(&sm.kv_full[g % kSlots], (g / kSlots) & 1, &sm.abort_flag, p.status, 134);
+          if (!(ok = __all_sync(0xffffffffu, ok))) break;
+          const int key = tid & 63;
+          if (clean_half_row<Type>(sm.kv[g % kSlots][tid >> 6], key)) {
+            if (t * kTileN + key < it.k_len) sm.special[nth & 1] = nth;
+            fence_proxy_async_smem();
+          }
+        }
         const int gk = load0 + 2 * t;
         ok = mbar_wait(&sm.done[gk % kSlots], (gk / kSlots) & 1, &sm.abort_flag, p.status, 130);
         if (!(ok = __all_sync(0xffffffffu, ok))) break;
@@ -370,7 +385,13 @@ attn_packed_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         tmem_ld32(tS, r0);
         tmem_ld32(tS + 32, r1);
         tmem_wait_ld();
-        if (t >= open_tiles) mask_columns_from(r0, r1, keys_of_row() - t * kTileN);
+        if (t >= open_tiles) {
+          // (the rows of a warp are neighbours: the mask's edge usually runs through one half of the columns)
+          const int valid = keys_of_row() - t * kTileN;
+          const int least = __reduce_min_sync(0xffffffffu, valid);
+          if (least < 32) mask_half(r0, valid);
+          if (least < 64) mask_half(r1, valid - 32);
+        }
         float2 sums = make_float2(0.f, 0.f);
         bool exact = st.m == -INFINITY;   // nothing accumulated yet: no reference maximum to try
         if (!__any_sync(0xffffffffu, exact)) {
@@ -407,17 +428,6 @@ attn_packed_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         st.l += sums.x + sums.y;
         tmem_st32(tS, pk);  // P_t over the first 32 columns of S_t
         tmem_wait_st();
-        if (t >= open_tiles) {
-          // some row of the item does not see all of these keys
-          const int g = load0 + 2 * t + 1;
-          ok = mbar_wait(&sm.kv_full[g % kSlots], (g / kSlots) & 1, &sm.abort_flag, p.status, 134);
-          if (!(ok = __all_sync(0xffffffffu, ok))) break;
-          const int key = tid & 63;
-          if (clean_half_row<Type>(sm.kv[g % kSlots][tid >> 6], key)) {
-            if (t * kTileN + key < it.k_len) sm.special[nth & 1] = nth;
-            fence_proxy_async_smem();
-          }
-        }
         tc_fence_before();
         mbar_arrive(&sm.p_full[buf]);
       }
@@ -455,20 +465,24 @@ attn_packed_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         }
       }
       __syncwarp();
-      // sixteen threads to a row's 256 bytes
-      const int64_t out = out_at();
-      const bool stored = row_valid();
+      // sixteen threads to a row's 256 bytes; the Q buffer is handed back as soon as the rows are in registers
+      uint4 x[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int from = 2 * i + (lane >> 4), r = warp * 32 + from;
-        const uint4 x = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(sm.q[(lane >> 3) & 1]) + r * 128 +
-                                                        (((lane & 7) ^ (r & 7)) << 4));
-        const int64_t to = __shfl_sync(0xffffffffu, out, from);
-        if (__shfl_sync(0xffffffffu, stored, from)) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + to + (lane & 15) * 8) = x;
+        const int r = warp * 32 + 2 * i + (lane >> 4);
+        x[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(sm.q[(lane >> 3) & 1]) + r * 128 +
+                                               (((lane & 7) ^ (r & 7)) << 4));
       }
       fence_proxy_async_smem();   // (the next Q comes through the async proxy)
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.q_free);
+      const bool stored = row_valid();
+      const int64_t out = stored ? out_at() : -1;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int64_t to = __shfl_sync(0xffffffffu, out, 2 * i + (lane >> 4));
+        if (to >= 0) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + to + (lane & 15) * 8) = x[i];
+      }
       if (p.lse != nullptr && stored) store_lse((st.m + log2f(st.l)) * 0.69314718055994531f);
       release_item();
       load0 += 2 * num_tiles;

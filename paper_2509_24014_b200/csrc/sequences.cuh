@@ -26,12 +26,14 @@ __device__ __forceinline__ void record_status(DeviceStatus* status, int code, in
   if (atomicCAS(&status->code, 0, code) == 0) status->where = where;
 }
 
-// The first and one past the last row of sequence b, clipped to [0, total].
-__device__ __forceinline__ int2 sequence_rows(const int32_t* cu, int b, int total, DeviceStatus* status, int where) {
-  const int first = __ldcg(cu + b), end = __ldcg(cu + b + 1);
+// The first and one past the last row of a sequence, clipped to [0, total].
+__device__ __forceinline__ int2 clip_rows(int first, int end, int total, DeviceStatus* status, int where) {
   const int f = min(max(first, 0), total), e = min(max(end, f), total);
   if (f != first || e != end) record_status(status, 6, where);
   return make_int2(f, e);
+}
+__device__ __forceinline__ int2 sequence_rows(const int32_t* cu, int b, int total, DeviceStatus* status, int where) {
+  return clip_rows(__ldcg(cu + b), __ldcg(cu + b + 1), total, status, where);
 }
 
 // Page of the cache that holds positions [place << page_shift, ...) of sequence b, or -1 where the table has none (recorded).
