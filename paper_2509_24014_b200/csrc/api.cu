@@ -1108,7 +1108,7 @@ extern "C" sparsed_status sparsed_cache_evict(const sparsed_cache* from, const f
   if (keep > static_cast<int64_t>(to->max_pages) * to->page_size) return SPARSED_ERR_INVALID_ARG;
   if (mass_capacity < static_cast<int64_t>(from->max_pages) * from->page_size || mass_out_capacity < keep)
     return SPARSED_ERR_INVALID_ARG;
-  if (static_cast<int64_t>(from->batch) * from->heads_kv * (keep / 64 + 1ll) > INT32_MAX) return SPARSED_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(from->batch) * from->heads_kv * (keep / 32 + 1ll) > INT32_MAX) return SPARSED_ERR_UNSUPPORTED;
   if (!aligned4(mass) || !aligned4(mass_out) || !aligned4(kept)) return SPARSED_ERR_ALIGNMENT;
   if ((st = check_ws(ws, ws_bytes, SPARSED_STATUS_BYTES)) != SPARSED_OK) return st;
   if ((st = check_arch()) != SPARSED_OK) return st;

@@ -63,19 +63,25 @@ __global__ void __launch_bounds__(32 * kWriteWarps) cache_write_kernel(const Cac
 
 // ------------------------------------------------------------------------------------------
 // Eviction, first half: which keys stay. A cluster of CTAs ranks one row (sequence, key-value head), each CTA a run of its
-// candidates (all but the `recent` last keys): radix selection of the (keep - recent)-th largest mass, 11 + 11 + 10 bits, over
-// histograms that the CTAs of the cluster read from each other; then every warp counts and writes out its share in order.
+// candidates (all but the `recent` last keys): radix selection of the (keep - recent)-th largest mass, 11 + 11 + 10 bits. Each
+// CTA counts its keys in a histogram of its own; then each adds up a slice of the bins over the cluster and scans it, and all
+// find the bin from the slices' totals (every CTA adding up every bin for itself took 2.5 us a step for a cluster of eight, 0.5
+// this way). At the end every warp counts and writes out its share in order. Bound by the latency of these steps.
 // ------------------------------------------------------------------------------------------
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectWarps = kSelectThreads / 32;
+constexpr int kMostRanks = 8;    // CTAs to a row
 constexpr int kBins = 2048;
+constexpr uint32_t kZeroKey = 0x80000000u;   // ordered_key(0)
 constexpr int kCachedKeys = 24 * 1024;   // of a CTA's run, held in shared memory (96 KB) as ordered keys
 
 struct EvictSmem {
   int hist[kBins];
+  int count[kBins], above[kBins];   // of this CTA's slice of the bins: keys in each over the cluster, and in the slice's bins above it
+  int slice_total;
   int warp_sum[kSelectWarps];
   int found_bin, found_above;
-  int above[kSelectWarps], equal[kSelectWarps];   // keys above / equal to the threshold in each warp's share
+  int keys_above[kSelectWarps], keys_equal[kSelectWarps];   // above / equal to the threshold in each warp's share
   int cta_above, cta_equal;
   uint32_t keys[kCachedKeys];
 };
@@ -87,6 +93,10 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
   wait_for_previous_kernel();
   cg::cluster_group cluster = cg::this_cluster();
   const int ranks = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
+  auto sync_row = [&]() {
+    if (ranks == 1) __syncthreads();
+    else cluster.sync();
+  };
   const int row = blockIdx.x / ranks;   // sequence * heads_kv + head
   const int seq = row / p.from.heads_kv, head = row % p.from.heads_kv;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -117,31 +127,43 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
   const int share = (candidates + ranks * kSelectWarps - 1) / (ranks * kSelectWarps);   // candidates per warp
   const int run0 = min(rank * kSelectWarps * share, candidates), run1 = min((rank + 1) * kSelectWarps * share, candidates);
   const int run = run1 - run0;
-  for (int i = tid; i < min(run, kCachedKeys); i += kSelectThreads) sm.keys[i] = ordered_key(__ldcg(mass + run0 + i));
+  const int cached = min(run, kCachedKeys);
+#pragma unroll 4
+  for (int i = tid; i < cached; i += kSelectThreads) sm.keys[i] = ordered_key(__ldcg(mass + run0 + i));
   auto key_at = [&](int i) -> uint32_t { return i < kCachedKeys ? sm.keys[i] : ordered_key(__ldcg(mass + run0 + i)); };
   // ---- the threshold -----------------------------------------------------------------------
   uint32_t prefix = 0u;
   int left = need;          // of the keys that agree with `prefix` in the bits decided so far
+  const int slice = kBins / ranks;   // bins that each CTA adds up: 2048, 1024, 512 or 256
   for (int step = 0; step < 3; ++step) {
     const int shift = step == 0 ? 21 : (step == 1 ? 10 : 0);
     const int bins = step == 2 ? 1024 : kBins;
     for (int i = tid; i < kBins; i += kSelectThreads) sm.hist[i] = 0;
     __syncthreads();
+    // Weights of exactly zero (keys that no query has looked at) are often most of a row: they are counted in registers, and
+    // not by thousands of additions to one place.
+    int zeros = 0;
     for (int i = tid; i < run; i += kSelectThreads) {
       const uint32_t key = key_at(i);
-      const bool in = step == 0 || (step == 1 ? (key >> 21) == (prefix >> 21) : (key >> 10) == (prefix >> 10));
-      if (in) atomicAdd(&sm.hist[(key >> shift) & (bins - 1)], 1);
+      const bool in = step == 0 || ((key ^ prefix) >> (shift + (step == 1 ? 11 : 10))) == 0u;
+      if (in && key == kZeroKey) ++zeros;
+      if (in && key != kZeroKey) atomicAdd(&sm.hist[(key >> shift) & (bins - 1)], 1);
     }
-    cluster.sync();
-    // bins from the top down, two to a thread: sums over the cluster, then a scan over the CTA
-    const int hi_bin = kBins - 1 - 2 * tid, lo_bin = hi_bin - 1;
-    int in_hi = 0, in_lo = 0;
-    for (int r = 0; r < ranks; ++r) {
-      const int2 two = *reinterpret_cast<const int2*>(cluster.map_shared_rank(&sm.hist[lo_bin], r));
-      in_lo += two.x;
-      in_hi += two.y;
+    zeros = __reduce_add_sync(0xffffffffu, zeros);
+    if (lane == 0 && zeros > 0) atomicAdd(&sm.hist[(kZeroKey >> shift) & (bins - 1)], zeros);
+    sync_row();
+    // This CTA's slice: the bins from rank * slice on, the highest first, two to a thread (one, where a slice has fewer).
+    const int per_thread = slice > kSelectThreads ? 2 : 1;
+    int hi = 0, lo = 0;
+    const int hi_bin = rank * slice + slice - 1 - per_thread * tid;   // (and the one below it)
+    const bool mine = per_thread * tid < slice;
+    if (mine) {
+#pragma unroll
+      for (int r = 0; r < kMostRanks; ++r)
+        if (r < ranks) hi += *cluster.map_shared_rank(&sm.hist[hi_bin], r);
+      if (per_thread == 2) lo = sm.hist[hi_bin - 1];   // (one CTA to the row)
     }
-    int sum = in_hi + in_lo;
+    int sum = hi + lo;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
       const int other = __shfl_up_sync(0xffffffffu, sum, d);
@@ -149,21 +171,39 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
     }
     if (lane == 31) sm.warp_sum[warp] = sum;
     __syncthreads();
-    int before = 0;
-    for (int w = 0; w < warp; ++w) before += sm.warp_sum[w];
-    const int above_lo = before + sum - in_lo, above_hi = above_lo - in_hi;   // keys in the bins above each of the two
-    if (above_hi < left && above_hi + in_hi >= left) {
-      sm.found_bin = hi_bin;
-      sm.found_above = above_hi;
+    sum += __reduce_add_sync(0xffffffffu, lane < warp ? sm.warp_sum[lane] : 0);
+    if (mine) {
+      const int at = hi_bin - rank * slice;
+      sm.count[at] = hi;
+      sm.above[at] = sum - lo - hi;
+      if (per_thread == 2) {
+        sm.count[at - 1] = lo;
+        sm.above[at - 1] = sum - lo;
+      }
     }
-    if (above_lo < left && above_lo + in_lo >= left) {
-      sm.found_bin = lo_bin;
-      sm.found_above = above_lo;
+    if (tid == kSelectThreads - 1) sm.slice_total = sum;
+    sync_row();
+    // The slice in which the count from the top passes `left`, then the bin: every CTA looks for itself.
+    const int total = lane < ranks ? *cluster.map_shared_rank(&sm.slice_total, ranks - 1 - lane) : 0;   // lane 0: the highest slice
+    int upto = total;
+#pragma unroll
+    for (int d = 1; d < kMostRanks; d *= 2) {
+      const int other = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += other;
     }
-    cluster.sync();   // (the histograms have been read; found_* are visible)
+    const int at_lane = __ffs(__ballot_sync(0xffffffffu, lane < ranks && upto >= left)) - 1;   // (the lowest reaches it at last)
+    const int owner = ranks - 1 - at_lane, before = __shfl_sync(0xffffffffu, upto - total, at_lane);
+    for (int i = tid; i < slice; i += kSelectThreads) {
+      const int above = before + *cluster.map_shared_rank(&sm.above[i], owner), in = *cluster.map_shared_rank(&sm.count[i], owner);
+      if (above < left && above + in >= left) {
+        sm.found_bin = owner * slice + i;
+        sm.found_above = above;
+      }
+    }
+    __syncthreads();
     prefix |= static_cast<uint32_t>(sm.found_bin) << shift;
     left -= sm.found_above;
-    __syncthreads();
+    // (count and above are read by other CTAs until they come to the next step's first barrier, and written behind it)
   }
   // Kept: keys above `prefix`, and the first `left` of those equal to it.
   // ---- where each warp's share goes ----------------------------------------------------------
@@ -177,27 +217,23 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
   above = __reduce_add_sync(0xffffffffu, above);
   equal = __reduce_add_sync(0xffffffffu, equal);
   if (lane == 0) {
-    sm.above[warp] = above;
-    sm.equal[warp] = equal;
+    sm.keys_above[warp] = above;
+    sm.keys_equal[warp] = equal;
   }
   __syncthreads();
   if (warp == 0) {
-    const int a = __reduce_add_sync(0xffffffffu, sm.above[lane]), e = __reduce_add_sync(0xffffffffu, sm.equal[lane]);
+    const int a = __reduce_add_sync(0xffffffffu, sm.keys_above[lane]), e = __reduce_add_sync(0xffffffffu, sm.keys_equal[lane]);
     if (lane == 0) {
       sm.cta_above = a;
       sm.cta_equal = e;
     }
   }
-  cluster.sync();
-  int above_before = 0, equal_before = 0;   // in the shares before this warp's
-  for (int r = 0; r < rank; ++r) {
-    above_before += *cluster.map_shared_rank(&sm.cta_above, r);
-    equal_before += *cluster.map_shared_rank(&sm.cta_equal, r);
-  }
-  for (int w = 0; w < warp; ++w) {
-    above_before += sm.above[w];
-    equal_before += sm.equal[w];
-  }
+  sync_row();
+  // in the shares before this warp's: those of CTAs before (a lane each) and of warps before
+  int above_before = lane < rank ? *cluster.map_shared_rank(&sm.cta_above, lane) : 0;
+  int equal_before = lane < rank ? *cluster.map_shared_rank(&sm.cta_equal, lane) : 0;
+  above_before = __reduce_add_sync(0xffffffffu, above_before + (lane < warp ? sm.keys_above[lane] : 0));
+  equal_before = __reduce_add_sync(0xffffffffu, equal_before + (lane < warp ? sm.keys_equal[lane] : 0));
   for (int i0 = my0; i0 < my1; i0 += 32) {
     const int i = i0 + lane;
     const uint32_t key = i < my1 ? key_at(i) : 0u;
@@ -213,52 +249,54 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
     above_before += __popc(a);
     equal_before += __popc(e);
   }
-  cluster.sync();   // no CTA leaves while another may still read its counts
+  sync_row();   // no CTA leaves while another may still read its counts
 }
 
 // ------------------------------------------------------------------------------------------
-// Eviction, second half: the kept rows of K and V to their new pages. Sixteen threads move a row; each has four rows of K and V
-// in flight.
+// Eviction, second half: the kept rows of K and V to their new pages. A warp moves 32 keys of a row: each lane looks up one
+// key's place and its new one, then sixteen lanes at a time move a key's 256 bytes, four keys of K and V in flight per lane.
 // ------------------------------------------------------------------------------------------
-constexpr int kMoveThreads = 256;
-constexpr int kMoveRows = 4;    // per sixteen threads
-constexpr int kMoveCta = kMoveThreads / 16 * kMoveRows;
+constexpr int kMoveThreads = 128;
 
 __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictParams p) {
   wait_for_previous_kernel();
-  const int ctas_per_row = (p.keep + kMoveCta - 1) / kMoveCta;
-  const int row = blockIdx.x / ctas_per_row, first = (blockIdx.x - row * ctas_per_row) * kMoveCta;
-  const int seq = row / p.from.heads_kv, head = row % p.from.heads_kv;
-  const int part = threadIdx.x >> 4, c = (threadIdx.x & 15) * 8;
-  const int32_t* kept = p.kept + static_cast<int64_t>(row) * p.keep;
-  uint4 kx[kMoveRows], vx[kMoveRows];
-  int from[kMoveRows];
-#pragma unroll
-  for (int i = 0; i < kMoveRows; ++i) {
-    const int j = first + i * (kMoveThreads / 16) + part;
-    from[i] = j < p.keep ? __ldcg(kept + j) : -1;
+  const int lane = threadIdx.x & 31, number = blockIdx.x * (kMoveThreads / 32) + (threadIdx.x >> 5);
+  const int warps_per_row = (p.keep + 31) / 32;
+  const int row = number / warps_per_row, j = (number - row * warps_per_row) * 32 + lane;
+  if (row >= p.from.batch * p.from.heads_kv) return;
+  const int seq = row / p.from.heads_kv, head = row - seq * p.from.heads_kv;
+  const int from = j < p.keep ? __ldcg(p.kept + static_cast<int64_t>(row) * p.keep + j) : -1;
+  int page = -1, new_page = -1;
+  if (from >= 0) {
+    new_page = page_of(p.to, seq, j >> p.to.page_shift, p.status, 10);
+    page = page_of(p.from, seq, from >> p.from.page_shift, p.status, 9);
   }
+  const int place = from & ((1 << p.from.page_shift) - 1), new_place = j & ((1 << p.to.page_shift) - 1);
+  const int c = (lane & 15) * 8;
+  const uint16_t* k = p.from.k + head * p.from.k_head + c;
+  const uint16_t* v = p.from.v + head * p.from.v_head + c;
+  uint16_t* new_k = p.to.k + head * p.to.k_head + c;
+  uint16_t* new_v = p.to.v + head * p.to.v_head + c;
+  for (int i0 = 0; i0 < 32; i0 += 8) {
+    if (__all_sync(0xffffffffu, lane < i0 || new_page < 0)) break;
+    uint4 kx[4], vx[4];
 #pragma unroll
-  for (int i = 0; i < kMoveRows; ++i) {
-    kx[i] = vx[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (from[i] >= 0) {
-      const int page = page_of(p.from, seq, from[i] >> p.from.page_shift, p.status, 9);
-      const int at = from[i] & ((1 << p.from.page_shift) - 1);
-      if (page >= 0) {
-        kx[i] = __ldcs(reinterpret_cast<const uint4*>(p.from.k + page * p.from.k_page + at * p.from.k_place + head * p.from.k_head + c));
-        vx[i] = __ldcs(reinterpret_cast<const uint4*>(p.from.v + page * p.from.v_page + at * p.from.v_place + head * p.from.v_head + c));
+    for (int i = 0; i < 4; ++i) {
+      const int key = i0 + 2 * i + (lane >> 4);
+      const int at_page = __shfl_sync(0xffffffffu, page, key), at = __shfl_sync(0xffffffffu, place, key);
+      kx[i] = vx[i] = make_uint4(0u, 0u, 0u, 0u);   // (a key whose page is missing comes over as zeros)
+      if (at_page >= 0) {
+        kx[i] = __ldcs(reinterpret_cast<const uint4*>(k + at_page * p.from.k_page + at * p.from.k_place));
+        vx[i] = __ldcs(reinterpret_cast<const uint4*>(v + at_page * p.from.v_page + at * p.from.v_place));
       }
     }
-  }
 #pragma unroll
-  for (int i = 0; i < kMoveRows; ++i) {
-    const int j = first + i * (kMoveThreads / 16) + part;
-    if (from[i] >= 0) {
-      const int page = page_of(p.to, seq, j >> p.to.page_shift, p.status, 10);
-      const int at = j & ((1 << p.to.page_shift) - 1);
-      if (page >= 0) {
-        *reinterpret_cast<uint4*>(p.to.k + page * p.to.k_page + at * p.to.k_place + head * p.to.k_head + c) = kx[i];
-        *reinterpret_cast<uint4*>(p.to.v + page * p.to.v_page + at * p.to.v_place + head * p.to.v_head + c) = vx[i];
+    for (int i = 0; i < 4; ++i) {
+      const int key = i0 + 2 * i + (lane >> 4);
+      const int to_page = __shfl_sync(0xffffffffu, new_page, key), to = __shfl_sync(0xffffffffu, new_place, key);
+      if (to_page >= 0) {
+        *reinterpret_cast<uint4*>(new_k + to_page * p.to.k_page + to * p.to.k_place) = kx[i];
+        *reinterpret_cast<uint4*>(new_v + to_page * p.to.v_page + to * p.to.v_place) = vx[i];
       }
     }
   }
@@ -280,7 +318,7 @@ cudaError_t launch_cache_evict(const EvictParams& p, cudaStream_t stream) {
   // As many CTAs to a row as fill the device, up to the portable cluster size, for rows long enough to be shared.
   const int room = p.from.max_pages << p.from.page_shift;
   int ranks = 1;
-  while (ranks < 8 && rows * ranks * 2 <= 148 && room / (2 * ranks) >= 2048) ranks *= 2;
+  while (ranks < kMostRanks && rows * ranks * 2 <= 148 && room / (2 * ranks) >= 2048) ranks *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(rows * ranks));
   cfg.blockDim = dim3(kSelectThreads);
@@ -290,12 +328,14 @@ cudaError_t launch_cache_evict(const EvictParams& p, cudaStream_t stream) {
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = static_cast<unsigned>(ranks);
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   e = cudaLaunchKernelEx(&cfg, evict_select_kernel, p);
   if (e == cudaSuccess) {
     cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>((p.keep + kMoveCta - 1) / kMoveCta * rows));
+    cfg.gridDim = dim3(static_cast<unsigned>((static_cast<int64_t>((p.keep + 31) / 32) * rows + kMoveThreads / 32 - 1) / (kMoveThreads / 32)));
     cfg.blockDim = dim3(kMoveThreads);
     cfg.stream = stream;
     attr[0] = {};
