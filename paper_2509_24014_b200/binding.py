@@ -119,12 +119,13 @@ def load_library() -> ctypes.CDLL:
     lib.sparsed_pattern_validate.argtypes = [P(Pattern), vp, sz, vp]
     lib.sparsed_last_device_status.argtypes = [vp, vp, P(i32), P(i32)]
     i64, f32 = ctypes.c_int64, ctypes.c_float
-    lib.sparsed_attn_packed.argtypes = [P(Packed), vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
-    lib.sparsed_cache_write.argtypes = [P(Cache), vp, P(i64), vp, P(i64), vp, i32, vp, sz, vp]
+    # (structures and strides of these are passed as addresses or as packed bytes)
+    lib.sparsed_attn_packed.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.sparsed_cache_write.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, sz, vp]
     lib.sparsed_paged_workspace_bytes.argtypes = [P(Cache), i32, i32, P(sz)]
-    lib.sparsed_attn_paged.argtypes = [P(Cache), i32, vp, P(i64), vp, P(i64), f32, vp, vp, vp, i64, vp, sz, vp]
+    lib.sparsed_attn_paged.argtypes = [vp, i32, vp, vp, vp, vp, f32, vp, vp, vp, i64, vp, sz, vp]
     lib.sparsed_evict_workspace_bytes.argtypes = [P(Cache), P(sz)]
-    lib.sparsed_cache_evict.argtypes = [P(Cache), vp, i64, i32, i32, P(Cache), vp, i64, vp, vp, sz, vp]
+    lib.sparsed_cache_evict.argtypes = [vp, vp, i64, i32, i32, vp, vp, i64, vp, vp, sz, vp]
     lib.sparsed_status_string.argtypes = [i32]
     lib.sparsed_status_string.restype = ctypes.c_char_p
     lib.sparsed_last_cuda_error.argtypes = []
@@ -412,23 +413,13 @@ def sparsed_last_device_status(ws: torch.Tensor) -> Tuple[int, int]:
 
 
 # ----------------------------------------------------------------------------- packed sequences and the paged cache
+# These calls are made for every layer and token, with little work behind some of them: their checks are single
+# expressions over values fetched once, and structures and strides go to the library as packed bytes.
 _DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_FP16}
 _PACKED_RECORD = struct.Struct("@8i8qf%dx" % (ctypes.sizeof(Packed) - struct.calcsize("@8i8qf")))
-_TwoStrides = ctypes.c_int64 * 2
-
-
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise ValueError(what)
-
-
-def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
-    """The device of all of them, as its index (-1: not a CUDA device)."""
-    device = first.get_device()
-    for t in others:
-        if t is not None and t.get_device() != device:
-            raise ValueError("all tensors of a call must be on the same device")
-    return device
+_TWO_STRIDES = struct.Struct("@2q")
+_int32, _fp32 = torch.int32, torch.float32
+_ELSEWHERE = "all tensors of a call must be on the same device"
 
 
 def _call(device: int, what: str, function, *args) -> None:
@@ -436,33 +427,31 @@ def _call(device: int, what: str, function, *args) -> None:
     if device < 0:
         raise ValueError(f"{what} needs CUDA tensors")
     stream = torch._C._cuda_getCurrentRawStream(device)
-    if device == torch.cuda.current_device():
-        _check(function(*args, stream), what)
+    if device == torch._C._cuda_getDevice():
+        status = function(*args, stream)
     else:
         with torch.cuda.device(device):
-            _check(function(*args, stream), what)
+            status = function(*args, stream)
+    if status != 0:
+        raise SparsedError(int(status), what)
 
 
-def _row_strides(t: torch.Tensor, heads: Optional[int], what: str) -> Tuple[int, int]:
+def _row_strides(shape, strides) -> Tuple[int, int]:
     """Strides (row, head) of a [rows, heads, 128] tensor. (A dimension of one or no rows may have any stride.)"""
-    shape, strides = t.shape, t.stride()
-    _need(len(shape) == 3 and (heads is None or shape[1] == heads), f"{what} must be [rows, heads, head_dim]")
-    _need(strides[2] == 1, f"{what}: head_dim must be contiguous")
     head = strides[1] if shape[1] > 1 else shape[2]
     return (strides[0] if shape[0] > 1 else max(shape[1] * shape[2], head)), head
 
 
-def _int32(t: torch.Tensor, dims: int, what: str) -> None:
-    _need(t.dtype == torch.int32 and t.dim() == dims and (t.shape[-1] <= 1 or t.stride(-1) == 1),
-          f"{what} must be int32 with {dims} dimension(s), the last one contiguous")
+def _offsets_ok(t: torch.Tensor, entries: int) -> bool:
+    return t.dtype is _int32 and t.shape == (entries,) and t.is_contiguous()
 
 
-def _fp32(t: Optional[torch.Tensor], shape, what: str) -> Optional[int]:
-    if t is None:
-        return None
-    _need(t.dtype == torch.float32 and t.is_contiguous() and (shape is None or tuple(t.shape) == tuple(shape)),
-          f"{what} must be fp32 and contiguous" + (f", {tuple(shape)}" if shape is not None else ""))
-    return t.data_ptr()
+def _fp32_ok(t: Optional[torch.Tensor], *shape) -> bool:
+    return t is None or (t.dtype is _fp32 and t.shape == shape and t.is_contiguous())
+
+
+def _pointer(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
 
 
 def sparsed_attn_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, cu_q: torch.Tensor,
@@ -471,33 +460,35 @@ def sparsed_attn_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: to
     """Attention over packed sequences: q, o [total_q, heads_q, 128], k, v [total_k, heads_kv, 128], bf16 or fp16;
     sequence b owns rows cu_q[b]:cu_q[b+1] of q and o and cu_k[b]:cu_k[b+1] of k and v (int32). With `causal` a sequence's
     queries are its last tokens. lse: fp32 [heads_q, total_q]. Rows behind the last sequence are left as they were."""
-    total_q, heads_q, head_dim = q.shape
-    total_k, heads_kv, _ = k.shape
-    device = _same_device(q, k, v, o, cu_q, cu_k, ws, lse)
-    _need(q.dtype in _DTYPES and q.dtype == k.dtype == v.dtype == o.dtype, "q, k, v, o must be all bf16 or all fp16")
-    _need(o.shape == q.shape and v.shape == k.shape and k.shape[2] == head_dim, "o must be shaped like q, v like k")
-    _int32(cu_q, 1, "cu_q")
-    _int32(cu_k, 1, "cu_k")
-    _need(cu_q.shape[0] == cu_k.shape[0] >= 1, "cu_q and cu_k must both be [num_seqs + 1]")
-    record = _PACKED_RECORD.pack(cu_q.shape[0] - 1, total_q, total_k, heads_q, heads_kv, head_dim, _DTYPES[q.dtype],
-                                 1 if causal else 0, *_row_strides(q, heads_q, "q"), *_row_strides(k, heads_kv, "k"),
-                                 *_row_strides(v, heads_kv, "v"), *_row_strides(o, heads_q, "o"), softmax_scale)
-    _call(device, "sparsed_attn_packed", load_library().sparsed_attn_packed, ctypes.byref(Packed.from_buffer_copy(record)),
-          cu_q.data_ptr(), cu_k.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
-          _fp32(lse, (heads_q, total_q), "lse"), ws.data_ptr(), ws.numel())
+    qs, ks, dtype, device = q.shape, k.shape, q.dtype, q.get_device()
+    qt, kt, vt, ot, entries = q.stride(), k.stride(), v.stride(), o.stride(), cu_q.shape[0]
+    if not (len(qs) == 3 == len(ks) and qs[2] == ks[2] and o.shape == qs and v.shape == ks and dtype in _DTYPES
+            and dtype is k.dtype is v.dtype is o.dtype and qt[2] == kt[2] == vt[2] == ot[2] == 1 and entries >= 1
+            and _offsets_ok(cu_q, entries) and _offsets_ok(cu_k, entries) and _fp32_ok(lse, qs[1], qs[0])):
+        raise ValueError("sparsed_attn_packed: q, o [total_q, heads_q, 128] and k, v [total_k, heads_kv, 128], all bf16 or "
+                         "all fp16, head_dim contiguous; cu_q, cu_k int32 [num_seqs + 1]; lse fp32 [heads_q, total_q]")
+    if not (device == k.get_device() == v.get_device() == o.get_device() == cu_q.get_device() == cu_k.get_device()
+            == ws.get_device() and (lse is None or lse.get_device() == device)):
+        raise ValueError(_ELSEWHERE)
+    record = _PACKED_RECORD.pack(entries - 1, qs[0], ks[0], qs[1], ks[1], qs[2], _DTYPES[dtype], 1 if causal else 0,
+                                 *_row_strides(qs, qt), *_row_strides(ks, kt), *_row_strides(ks, vt),
+                                 *_row_strides(qs, ot), softmax_scale)
+    _call(device, "sparsed_attn_packed", (_lib or load_library()).sparsed_attn_packed, record, cu_q.data_ptr(),
+          cu_k.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _pointer(lse), ws.data_ptr(), ws.numel())
 
 
 def make_cache(k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor) -> Cache:
     """A paged key-value cache: pools k, v [num_pages, page_size, heads_kv, 128] (any strides with head_dim contiguous, so a
     transposed view of [num_pages, heads_kv, page_size, 128] too), page_table int32 [batch, max_pages], seq_lens int32
     [batch]. The calls read the tensors' contents when they run; make it once and keep it."""
-    _need(k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.dtype in _DTYPES,
-          "k and v must be [num_pages, page_size, heads_kv, head_dim], bf16 or fp16")
-    _need(k.stride(3) == 1 and v.stride(3) == 1, "head_dim must be contiguous")
-    _int32(page_table, 2, "page_table")
-    _int32(seq_lens, 1, "seq_lens")
-    _need(page_table.shape[0] == seq_lens.shape[0], "page_table and seq_lens must have the same batch")
-    _same_device(k, v, page_table, seq_lens)
+    device = k.get_device()
+    if not (k.dim() == 4 and k.shape == v.shape and k.dtype is v.dtype and k.dtype in _DTYPES
+            and k.stride(3) == 1 == v.stride(3) and page_table.dim() == 2 and page_table.dtype is _int32
+            and (page_table.shape[1] <= 1 or page_table.stride(1) == 1) and _offsets_ok(seq_lens, page_table.shape[0])):
+        raise ValueError("make_cache: k, v [num_pages, page_size, heads_kv, 128], both bf16 or fp16, head_dim contiguous; "
+                         "page_table int32 [batch, max_pages], rows contiguous; seq_lens int32 [batch]")
+    if not device == v.get_device() == page_table.get_device() == seq_lens.get_device():
+        raise ValueError(_ELSEWHERE)
 
     def strides(t):   # a dimension of one place may have any stride
         head = t.stride(2) if t.shape[2] > 1 else t.shape[3]
@@ -508,6 +499,7 @@ def make_cache(k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, seq_l
               (ctypes.c_int64 * 3)(*strides(v)), k.shape[0], k.shape[1], k.shape[2], k.shape[3], page_table.shape[0],
               page_table.shape[1], _DTYPES[k.dtype])
     c.tensors = (k, v, page_table, seq_lens)
+    c.device, c.type, c.place, c.rows = device, k.dtype, ctypes.addressof(c), (page_table.shape[0], k.shape[2])
     return c
 
 
@@ -515,17 +507,16 @@ def sparsed_cache_write(cache: Cache, k_new: torch.Tensor, v_new: torch.Tensor, 
                         ws: torch.Tensor) -> None:
     """New tokens' keys and values [total_new, heads_kv, 128] to the last positions of their sequences (seq_lens counts them
     already); sequence b's are rows cu_new[b]:cu_new[b+1]."""
-    pool = cache.tensors[0]
-    device = _same_device(pool, k_new, v_new, cu_new, ws)
-    _need(k_new.dtype == v_new.dtype == pool.dtype, "k_new and v_new must have the cache's type")
-    _need(k_new.shape == v_new.shape and k_new.dim() == 3 and k_new.shape[2] == cache.head_dim,
-          "k_new and v_new must be [total_new, heads_kv, head_dim]")
-    _int32(cu_new, 1, "cu_new")
-    _need(cu_new.shape[0] == cache.batch + 1, "cu_new must be [batch + 1]")
-    _call(device, "sparsed_cache_write", load_library().sparsed_cache_write, ctypes.byref(cache), k_new.data_ptr(),
-          _TwoStrides(*_row_strides(k_new, cache.heads_kv, "k_new")), v_new.data_ptr(),
-          _TwoStrides(*_row_strides(v_new, cache.heads_kv, "v_new")), cu_new.data_ptr(), k_new.shape[0], ws.data_ptr(),
-          ws.numel())
+    shape, kt, vt, device, (batch, heads_kv) = k_new.shape, k_new.stride(), v_new.stride(), cache.device, cache.rows
+    if not (len(shape) == 3 and shape[1] == heads_kv and shape[2] == 128 and v_new.shape == shape and kt[2] == 1 == vt[2]
+            and k_new.dtype is v_new.dtype is cache.type and _offsets_ok(cu_new, batch + 1)):
+        raise ValueError("sparsed_cache_write: k_new, v_new [total_new, heads_kv, 128] of the cache's type, head_dim "
+                         "contiguous; cu_new int32 [batch + 1]")
+    if not device == k_new.get_device() == v_new.get_device() == cu_new.get_device() == ws.get_device():
+        raise ValueError(_ELSEWHERE)
+    _call(device, "sparsed_cache_write", (_lib or load_library()).sparsed_cache_write, cache.place, k_new.data_ptr(),
+          _TWO_STRIDES.pack(*_row_strides(shape, kt)), v_new.data_ptr(), _TWO_STRIDES.pack(*_row_strides(shape, vt)),
+          cu_new.data_ptr(), shape[0], ws.data_ptr(), ws.numel())
 
 
 def sparsed_paged_workspace_bytes(cache: Cache, heads_q: int, with_mass: bool = False) -> int:
@@ -541,21 +532,22 @@ def sparsed_attn_paged(q: torch.Tensor, cache: Cache, o: torch.Tensor, ws: torch
     """One new token per sequence, q, o [batch, heads_q, 128], over its cached keys. lse: fp32 [batch, heads_q].
     mass_out: fp32 [batch, heads_kv, capacity], receives mass_in (the same tensor, another, or None: zeros) plus each cached
     key's attention weight, summed over the query heads of its group."""
-    batch, heads_q, head_dim = q.shape
-    pool = cache.tensors[0]
-    device = _same_device(pool, q, o, ws, lse, mass_in, mass_out)
-    _need(q.dtype == o.dtype == pool.dtype, "q and o must have the cache's type")
-    _need(batch == cache.batch and head_dim == cache.head_dim and o.shape == q.shape, "q and o must be [batch, heads_q, head_dim]")
-    capacity, in_ptr, out_ptr = 0, None, None
-    if mass_out is not None or mass_in is not None:
-        _need(mass_out is not None, "mass_in needs mass_out")
-        _need(mass_out.dim() == 3, "mass_out must be [batch, heads_kv, capacity]")
-        capacity = mass_out.shape[2]
-        in_ptr = _fp32(mass_in, (batch, cache.heads_kv, capacity), "mass_in")
-        out_ptr = _fp32(mass_out, (batch, cache.heads_kv, capacity), "mass_out")
-    _call(device, "sparsed_attn_paged", load_library().sparsed_attn_paged, ctypes.byref(cache), heads_q, q.data_ptr(),
-          _TwoStrides(*_row_strides(q, heads_q, "q")), o.data_ptr(), _TwoStrides(*_row_strides(o, heads_q, "o")),
-          softmax_scale, _fp32(lse, (batch, heads_q), "lse"), in_ptr, out_ptr, capacity, ws.data_ptr(), ws.numel())
+    shape, qt, ot, device, (batch, heads_kv) = q.shape, q.stride(), o.stride(), cache.device, cache.rows
+    ok = (len(shape) == 3 and shape[0] == batch and shape[2] == 128 and o.shape == shape and qt[2] == 1 == ot[2]
+          and q.dtype is o.dtype is cache.type and _fp32_ok(lse, batch, shape[1]))
+    capacity = 0
+    if mass_out is not None:
+        capacity = mass_out.shape[-1]
+        ok = ok and _fp32_ok(mass_out, batch, heads_kv, capacity) and _fp32_ok(mass_in, batch, heads_kv, capacity)
+    if not ok or (mass_in is not None and mass_out is None):
+        raise ValueError("sparsed_attn_paged: q, o [batch, heads_q, 128] of the cache's type, head_dim contiguous; lse fp32 "
+                         "[batch, heads_q]; mass_out, mass_in (only with mass_out) fp32 [batch, heads_kv, capacity]")
+    if not (device == q.get_device() == o.get_device() == ws.get_device() and (lse is None or lse.get_device() == device)
+            and (mass_out is None or mass_out.get_device() == device) and (mass_in is None or mass_in.get_device() == device)):
+        raise ValueError(_ELSEWHERE)
+    _call(device, "sparsed_attn_paged", (_lib or load_library()).sparsed_attn_paged, cache.place, shape[1], q.data_ptr(),
+          _TWO_STRIDES.pack(*_row_strides(shape, qt)), o.data_ptr(), _TWO_STRIDES.pack(*_row_strides(shape, ot)),
+          softmax_scale, _pointer(lse), _pointer(mass_in), _pointer(mass_out), capacity, ws.data_ptr(), ws.numel())
 
 
 def sparsed_evict_workspace_bytes(cache: Cache) -> int:
@@ -570,12 +562,13 @@ def sparsed_cache_evict(cache: Cache, mass: torch.Tensor, keep: int, recent: int
     """Moves, for every sequence and key-value head, the `recent` last keys and those with the largest mass, min(keep, length)
     in all, in their order, to the pages of `to`, whose seq_lens are written. mass: fp32 [batch, heads_kv, capacity];
     mass_out: fp32 [batch, heads_kv, new capacity]; kept: int32 [batch, heads_kv, keep], the kept positions, then -1."""
-    device = _same_device(cache.tensors[0], to.tensors[0], mass, mass_out, kept, ws)
-    _need(mass.dim() == 3 and mass_out.dim() == 3, "mass and mass_out must be [batch, heads_kv, capacity]")
-    rows = (cache.batch, cache.heads_kv)
-    _need(kept.dtype == torch.int32 and kept.is_contiguous() and tuple(kept.shape) == rows + (keep,),
-          "kept must be int32 and contiguous, [batch, heads_kv, keep]")
-    _call(device, "sparsed_cache_evict", load_library().sparsed_cache_evict, ctypes.byref(cache),
-          _fp32(mass, rows + (mass.shape[2],), "mass"), mass.shape[2], int(keep), int(recent), ctypes.byref(to),
-          _fp32(mass_out, rows + (mass_out.shape[2],), "mass_out"), mass_out.shape[2], kept.data_ptr(), ws.data_ptr(),
-          ws.numel())
+    device, (batch, heads_kv) = cache.device, cache.rows
+    if not (_fp32_ok(mass, batch, heads_kv, mass.shape[-1]) and _fp32_ok(mass_out, batch, heads_kv, mass_out.shape[-1])
+            and kept.dtype is _int32 and kept.shape == (batch, heads_kv, keep) and kept.is_contiguous()):
+        raise ValueError("sparsed_cache_evict: mass, mass_out fp32 [batch, heads_kv, capacity], kept int32 [batch, heads_kv, "
+                         "keep], all contiguous")
+    if not device == to.device == mass.get_device() == mass_out.get_device() == kept.get_device() == ws.get_device():
+        raise ValueError(_ELSEWHERE)
+    _call(device, "sparsed_cache_evict", (_lib or load_library()).sparsed_cache_evict, cache.place, mass.data_ptr(),
+          mass.shape[-1], int(keep), int(recent), to.place, mass_out.data_ptr(), mass_out.shape[-1], kept.data_ptr(),
+          ws.data_ptr(), ws.numel())
