@@ -396,7 +396,7 @@ attn_packed_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         bool exact = st.m == -INFINITY;   // nothing accumulated yet: no reference maximum to try
         if (!__any_sync(0xffffffffu, exact)) {
           sums = softmax_group_fast<Type>(r0, r1, scale_log2, st.m, pk);
-          exact = sums.x + sums.y > 256.0f;   // logits outgrew the running maximum (a NaN makes the row NaN either way)
+          exact = sums.x + sums.y > static_cast<float>(1u << static_cast<int>(Type::kSlack));   // logits outgrew the running maximum (a NaN makes the row NaN either way)
         }
         if (__any_sync(0xffffffffu, exact)) {
           // Rows whose reference has to move take their own maximum of the tile; the others keep theirs and get the same P

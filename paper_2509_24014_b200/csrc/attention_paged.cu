@@ -36,7 +36,6 @@ constexpr int kWarpKeys = 16;
 constexpr int kUnit = kWarps * kWarpKeys;
 constexpr int kTileBytes = kWarpKeys * kHeadDim * 2;
 constexpr int kMostCtas = 1024;
-constexpr float kSlack = 8.f;   // a probability may outgrow its reference to 2^8 before the reference moves
 
 template <class Type>
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -283,7 +282,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 #pragma unroll
         for (int n = 0; n < kNT; ++n)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) outgrown = outgrown || fmaxf(s[n][x], s[n][x + 2]) > m[n][x] + kSlack;
+          for (int x = 0; x < 2; ++x) outgrown = outgrown || fmaxf(s[n][x], s[n][x + 2]) > m[n][x] + Type::kSlack;
         if constexpr (kMass) {
 #pragma unroll
           for (int n = 0; n < kNT; ++n)
@@ -302,7 +301,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-              if (top > m[n][x] + kSlack) {   // (a head's result does not depend on the other heads)
+              if (top > m[n][x] + Type::kSlack) {   // (a head's result does not depend on the other heads)
                 const float alpha = fast_exp2(m[n][x] - top);   // 0 when nothing was accumulated yet
                 m[n][x] = top;
                 l[n][x] *= alpha;

@@ -18,7 +18,11 @@
 namespace sparsed {
 
 // The 16-bit type of Q, K, V, P and O. (Most calls take bf16 only; the packed ones fp16 too.)
+// kSlack: how far (base 2) a row's sum over a tile may outgrow the reference in use before the reference is moved. P's relative
+// precision does not depend on it: with bf16 it is bounded by what P * V may reach in fp32 (2^24 leaves V 2^103), with fp16 by
+// P itself (2^16). (Most calls' kernels move it from 2^8 on, which costs them little on the inputs they were measured with.)
 struct Bf16Type {
+  static constexpr float kSlack = 24.f;
   static constexpr uint32_t kExponents = 0x7f807f80u;     // exponent bits of a pair
   static constexpr uint32_t kExponentCarry = 0x00800080u; // added to them: bit 15 / 31 is set where all were ones
   static __host__ __device__ constexpr uint32_t idesc(uint32_t bf16) { return bf16; }
@@ -28,6 +32,7 @@ struct Bf16Type {
   }
 };
 struct Fp16Type {
+  static constexpr float kSlack = 15.f;
   static constexpr uint32_t kExponents = 0x7c007c00u;
   static constexpr uint32_t kExponentCarry = 0x04000400u;
   static __host__ __device__ constexpr uint32_t idesc(uint32_t bf16) { return bf16 & ~((1u << 7) | (1u << 10)); }   // both formats 0: fp16
