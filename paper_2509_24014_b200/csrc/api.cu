@@ -867,6 +867,19 @@ sparsed_status check_scale(float scale, float* scale_log2) {
   return SPARSED_OK;
 }
 
+// Whether a packed call runs on the CTA-pair kernel. SPARSED_PACKED_KERNEL=pair|single (read once) sends every call to one of the
+// two, for measurements and tests.
+bool packed_kernel_is_pair(const sparsed_packed* s, int pack, int tile_tokens) {
+  static const int forced = [] {
+    const char* v = std::getenv("SPARSED_PACKED_KERNEL");
+    if (v != nullptr && std::strcmp(v, "pair") == 0) return 1;
+    if (v != nullptr && std::strcmp(v, "single") == 0) return 0;
+    return -1;
+  }();
+  if (forced >= 0) return forced == 1;
+  return packed_pair_pays(s->num_seqs, s->total_q, s->total_k, s->heads_q / pack, tile_tokens, s->causal != 0);
+}
+
 // The sizes of a cache alone (what the workspace queries need).
 sparsed_status check_cache_sizes(const sparsed_cache* c) {
   if (c == nullptr) return SPARSED_ERR_INVALID_ARG;
@@ -939,8 +952,9 @@ extern "C" sparsed_status sparsed_attn_packed(const sparsed_packed* shape, const
   p.group = shape->heads_q / shape->heads_kv;
   p.pack = packed_heads_per_tile(p.group);
   p.tile_tokens = 128 / p.pack;
-  const int64_t tiles = static_cast<int64_t>(shape->total_q) / p.tile_tokens + shape->num_seqs;
-  if (tiles * (shape->heads_q / p.pack) > INT32_MAX) return SPARSED_ERR_UNSUPPORTED;
+  const bool pair = packed_kernel_is_pair(shape, p.pack, p.tile_tokens);
+  const int64_t tiles = static_cast<int64_t>(shape->total_q) / (pair ? 4 * p.tile_tokens : p.tile_tokens) + shape->num_seqs;
+  if (tiles * (shape->heads_q / p.pack) > INT32_MAX / 2) return SPARSED_ERR_UNSUPPORTED;
   const bool nothing = shape->num_seqs == 0 || shape->total_q == 0, no_keys = shape->total_k == 0;
   if (cu_q == nullptr || cu_k == nullptr) return SPARSED_ERR_INVALID_ARG;
   if (!nothing && (q == nullptr || o == nullptr)) return SPARSED_ERR_INVALID_ARG;
@@ -958,7 +972,7 @@ extern "C" sparsed_status sparsed_attn_packed(const sparsed_packed* shape, const
   if (no_keys) {
     tk = tv = tq;   // (nothing is loaded through them)
   } else {
-    if ((st = make_tensor_map(&tk, k, 1, shape->heads_kv, shape->total_k, k3, 64)) != SPARSED_OK) return st;
+    if ((st = make_tensor_map(&tk, k, 1, shape->heads_kv, shape->total_k, k3, pair ? 32 : 64)) != SPARSED_OK) return st;
     if ((st = make_tensor_map(&tv, v, 1, shape->heads_kv, shape->total_k, v3, 64)) != SPARSED_OK) return st;
   }
   p.cu_q = cu_q;
@@ -983,7 +997,8 @@ extern "C" sparsed_status sparsed_attn_packed(const sparsed_packed* shape, const
   p.max_ctas = attn_max_ctas();
   p.slow_path_events = reinterpret_cast<unsigned long long*>(static_cast<uint8_t*>(ws) + 32);
   p.status = static_cast<DeviceStatus*>(ws);
-  cudaError_t e = launch_attn_packed(tq, tk, tv, p, shape->dtype == SPARSED_DTYPE_FP16, static_cast<cudaStream_t>(cuda_stream));
+  auto launch = pair ? launch_attn_packed_pair : launch_attn_packed;
+  cudaError_t e = launch(tq, tk, tv, p, shape->dtype == SPARSED_DTYPE_FP16, static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? SPARSED_OK : cuda_fail(e);
 }
 

@@ -26,9 +26,7 @@
 //
 // Bound: as the dense kernel, the tensor pipe and the softmax warps at the power limit; short sequences by what an item costs
 // beside its tiles.
-#include "internal.h"
-#include "sequences.cuh"
-#include "softmax_pipeline.cuh"
+#include "packed_rows.cuh"
 #include "work_items.cuh"
 
 namespace sparsed {
@@ -43,13 +41,10 @@ constexpr int kColO = 128;    // O accumulator (fp32, 128 columns)
 constexpr int kSlots = 5;
 
 // What the roles of a CTA need to know of an item.
-struct PackedItem {
+struct PackedItem : PackedTokens {
   int num_tiles;     // 64-key tiles to walk; -1: no more items
   int open_tiles;    // the first of them, all of whose keys all rows see
-  int q_row, tokens; // first row of q and o, and how many tokens the item has
   int head;          // first query head
-  int first_keys;    // causal: keys that the first token sees (may be negative), one more for each later one
-  int k_row, k_len;  // the sequence's keys
 };
 
 struct PackedSmem {
@@ -67,33 +62,6 @@ struct PackedSmem {
   int abort_flag;
   int special[2];          // number of the item in whose masked tiles a V of its sequence is infinite or NaN
 };
-
-// Makes what is not finite in this thread's half row of a 64 x 128 tile of V zero. Returns whether there was any.
-template <class Type>
-__device__ __forceinline__ bool clean_half_row(uint16_t* half_tile, int row) {
-  uint4* chunks = reinterpret_cast<uint4*>(half_tile + row * 64);
-  uint32_t found = 0;
-#pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    const uint4 x = chunks[(c + row) & 7];   // (rotated: rows are 128 bytes apart; the swizzle does not matter here)
-    found |= non_finite_pair<Type>(x.x) | non_finite_pair<Type>(x.y) | non_finite_pair<Type>(x.z) | non_finite_pair<Type>(x.w);
-  }
-  if (found == 0u) return false;
-  uint32_t* words = reinterpret_cast<uint32_t*>(chunks);
-  for (int i = 0; i < 32; ++i) {
-    const uint32_t bad = non_finite_pair<Type>(words[i]);
-    if (bad & 0x8000u) words[i] &= 0xffff0000u;
-    if (bad & 0x80000000u) words[i] &= 0x0000ffffu;
-  }
-  return true;
-}
-
-// -inf in the columns at and beyond `valid` of 32
-__device__ __forceinline__ void mask_half(uint32_t (&r)[32], int valid) {
-#pragma unroll
-  for (int j = 0; j < 32; ++j)
-    if (j >= valid) r[j] = 0xff800000u;
-}
 
 template <class Type>
 __global__ void __launch_bounds__(kThreads, 2)
@@ -146,30 +114,14 @@ attn_packed_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   // Warps 4 and 5 run their loops with all 32 lanes converged and let one elected lane issue.
   if (warp == 4) {
     // =============================== producer ===========================================
-    // Heads are taken heads_per_pass at a time (their K and V stay in L2), tiles from the last one down: with a causal mask a
-    // sequence's last tiles are its longest.
-    const int packed_heads = p.heads_q / p.pack, per_pass = p.tiles * p.heads_per_pass;
     PackedItem it;
     // what grid number `number` is; false: an empty tile
     auto describe = [&](int number) -> bool {
-      const int pass = number / per_pass, in_pass = number - pass * per_pass;
-      const int heads_here = min(p.heads_per_pass, packed_heads - pass * p.heads_per_pass);
-      const int tile = p.tiles - 1 - in_pass / heads_here;
-      it.head = (pass * p.heads_per_pass + in_pass % heads_here) * p.pack;
-      const int seq = last_not_above(p.num_seqs, tile, [&](int b) { return __ldcg(p.cu_q + b) / p.tile_tokens + b; });
-      const int2 q_rows = sequence_rows(p.cu_q, seq, p.total_q, p.status, 4);
-      const int2 k_rows = sequence_rows(p.cu_k, seq, p.total_k, p.status, 5);
-      const int q_len = q_rows.y - q_rows.x;
-      const int q0 = (tile - (q_rows.x / p.tile_tokens + seq)) * p.tile_tokens;   // the tile's first token in its sequence
-      if (q0 < 0 || q0 >= q_len) return false;
-      it.q_row = q_rows.x + q0;
-      it.tokens = min(p.tile_tokens, q_len - q0);
-      it.k_row = k_rows.x;
-      it.k_len = k_rows.y - k_rows.x;
-      it.first_keys = p.causal ? q0 + 1 + it.k_len - q_len : it.k_len;
-      const int seen = p.causal ? min(max(it.first_keys + it.tokens - 1, 0), it.k_len) : it.k_len;
-      it.num_tiles = (seen + kTileN - 1) / kTileN;
-      it.open_tiles = min(max(it.first_keys, 0), it.k_len) / kTileN;
+      const int2 tile_head = packed_tile_and_head(p, number);
+      if (!packed_tokens(p, tile_head.x, p.tile_tokens, it)) return false;
+      it.head = tile_head.y * p.pack;
+      it.num_tiles = (it.keys_of(it.tokens - 1, p.causal) + kTileN - 1) / kTileN;
+      it.open_tiles = it.keys_of(0, p.causal) / kTileN;
       return true;
     };
     auto request_item = [&]() {
@@ -360,7 +312,7 @@ attn_packed_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         continue;
       }
       // keys this row sees
-      auto keys_of_row = [&]() -> int { return p.causal ? min(max(it.first_keys + token, 0), it.k_len) : it.k_len; };
+      auto keys_of_row = [&]() -> int { return it.keys_of(token, p.causal); };
       // (a row that is nobody's holds anything: a finite reference keeps it from asking for the exact path in every tile)
       RowState st{row_valid() ? -INFINITY : 0.f, 0.f};
       for (int t = 0; t < num_tiles; ++t) {
@@ -370,7 +322,8 @@ attn_packed_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           ok = mbar_wait(&sm.kv_full[g % kSlots], (g / kSlots) & 1, &sm.abort_flag, p.status, 134);
           if (!(ok = __all_sync(0xffffffffu, ok))) break;
           const int key = tid & 63;
-          if (clean_half_row<Type>(sm.kv[g % kSlots][tid >> 6], key)) {
+          if (has_non_finite<Type>(sm.kv[g % kSlots][tid >> 6], key)) {
+            clean_half_row<Type>(sm.kv[g % kSlots][tid >> 6], key);
             if (t * kTileN + key < it.k_len) sm.special[nth & 1] = nth;
             fence_proxy_async_smem();
           }
@@ -445,44 +398,17 @@ attn_packed_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       tc_fence_before();   // the next item's first P V overwrites O: order these reads before its hand-over
       // (all threads wrote their notes before the hand-over of the P whose P V has just been waited for)
       if (*reinterpret_cast<volatile int*>(&sm.special[nth & 1]) == nth && row_valid()) {
-        // what was taken out of V in the masked tiles: a probability times an infinity or NaN is that infinity or NaN
-        const int kv_head = it.head / p.group, row_keys = keys_of_row();
-        for (int d = 0; d < kHeadDim; d += 2) {
-          uint32_t* at = reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(sm.q[d >> 6]) + tid * 128 +
-                                                     ((((d & 63) >> 3) ^ (tid & 7)) << 4) + (d & 7) * 2);
-          float2 sum = Type::unpack(*at);
-          bool any = false;
-          for (int j = it.open_tiles * kTileN; j < row_keys; ++j) {
-            const uint32_t x = __ldcg(reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p.v) +
-                                                                        (it.k_row + j) * p.v_stride_t + kv_head * p.v_stride_h + d));
-            const uint32_t bad = non_finite_pair<Type>(x);
-            const float2 f = Type::unpack(x);
-            if (bad & 0x8000u) sum.x += f.x;
-            if (bad & 0x80000000u) sum.y += f.y;
-            any = any || bad != 0u;
-          }
-          if (any) *at = Type::pack(sum.x, sum.y);
-        }
+        add_special<Type>(p, sm.q, tid, it.k_row, open_tiles * kTileN, keys_of_row(), it.head / p.group);
       }
       __syncwarp();
-      // sixteen threads to a row's 256 bytes; the Q buffer is handed back as soon as the rows are in registers
+      // the Q buffer is handed back as soon as the rows are in registers
       uint4 x[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int r = warp * 32 + 2 * i + (lane >> 4);
-        x[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(sm.q[(lane >> 3) & 1]) + r * 128 +
-                                               (((lane & 7) ^ (r & 7)) << 4));
-      }
+      read_staged_rows(sm.q, warp * 32, lane, x);
       fence_proxy_async_smem();   // (the next Q comes through the async proxy)
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.q_free);
       const bool stored = row_valid();
-      const int64_t out = stored ? out_at() : -1;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int64_t to = __shfl_sync(0xffffffffu, out, 2 * i + (lane >> 4));
-        if (to >= 0) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + to + (lane & 15) * 8) = x[i];
-      }
+      store_rows(p.o, stored ? out_at() : -1, lane, x);
       if (p.lse != nullptr && stored) store_lse((st.m + log2f(st.l)) * 0.69314718055994531f);
       release_item();
       load0 += 2 * num_tiles;

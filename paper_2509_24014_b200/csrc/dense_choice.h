@@ -81,6 +81,27 @@ inline DenseKernel choose_dense_kernel(bool with_stats, long long bh, int seq_le
   return with_stats || dense_pair_pays(bh, seq_len, max_ctas) ? DenseKernel::kPair : DenseKernel::kSingle;
 }
 
+// Whether attention over packed sequences goes to the kernel whose MMAs span CTA pairs (attention_packed_pair.cu): four tiles of
+// `tile_tokens` tokens to a cluster. The lengths are only known on the device, so this goes by their averages.
+// Beside the keys that rows see (`keys`, on average), a cluster pays for its set-up, about 200 keys' worth, and with a causal mask
+// for the keys that only its last tokens see, half of its tokens on average, where a CTA of the other kernel pays for half of a
+// tile's. Per key it takes 0.905 of the other's time under sustained load (0.91 after a rest). Measured, pair over single, after
+// a rest | sustained: no mask, 8 x 2048 x 32 heads 1.00 | 1.00, 4 x 4096 0.94 | 0.95, 2 x 8192 0.92 | 0.92, 16384 0.90 | 0.91;
+// causal, 2 x 8192 0.99 | 0.99, 12288 0.95 | 0.97, 16384 0.94 | 0.95, 32768 0.92 | 0.94, 28 heads on 4, 5000 + 9000 + 3000
+// 0.97 | 0.96, 4 x 2048 on 8192 cached 0.92 | 0.91. Few clusters: no mask, 8192 x 2 heads (32 clusters) 1.07 | 1.11, x 3 (48)
+// 0.95 | 0.96, x 5 (80) 0.99 | 0.99; causal, whose last clusters are the longest, 32768 x 1 head (64) 1.08 | 1.10, x 2 (128)
+// 0.93 | 0.92. Mixed lengths are judged by less than they are: 9000 + 2000 + 700 + 5000 x 32 causal 1.03 | 1.09 stays.
+inline bool packed_pair_pays(long long num_seqs, long long total_q, long long total_k, int packed_heads, int tile_tokens,
+                             bool causal) {
+  if (num_seqs < 1) return false;
+  const double avg_q = static_cast<double>(total_q) / num_seqs, avg_k = static_cast<double>(total_k) / num_seqs;
+  if (avg_q < 4.0 * tile_tokens) return false;
+  const double clusters = avg_q / (4.0 * tile_tokens) * num_seqs * packed_heads;
+  if (clusters < (causal ? 128.0 : 48.0)) return false;
+  const double keys = causal ? avg_k - 0.5 * avg_q : avg_k;
+  return 0.905 * (keys + 200.0 + (causal ? 2.0 * tile_tokens : 0.0)) < 0.98 * (keys + (causal ? 0.5 * tile_tokens : 0.0));
+}
+
 // lone_ctas_pay for block-sparse attention. Alone, the lists may be of any length: 2 heads x 1024 block 128, one block a row
 // 5.85 -> 5.56, six 12.3 -> 10.5; 16 x 512 block 32 (walked as the union of four rows' lists) one 7.72 -> 7.15, ten 11.9
 // -> 10.4; 2 x 4096 block 32, twelve 21.8 -> 16.3; no blocks at all, 8 x 1024 block 32, 4.2 -> 3.7; one whole row among

@@ -33,6 +33,11 @@ int packed_heads_per_tile(int group);
 cudaError_t launch_attn_packed(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const PackedParams& p,
                                bool fp16, cudaStream_t stream);
 
+// The same with the MMAs spanning CTA pairs (attention_packed_pair.cu): p.tiles counts tiles of 4 * p.tile_tokens tokens, K's
+// boxes are 64 x 32 rows.
+cudaError_t launch_attn_packed_pair(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const PackedParams& p,
+                                    bool fp16, cudaStream_t stream);
+
 // A paged cache as the kernels see it (16-bit elements).
 struct CacheView {
   uint16_t *k, *v;

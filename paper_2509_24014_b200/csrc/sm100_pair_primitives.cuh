@@ -37,6 +37,10 @@ __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t cluster_addr) {
   return v;
 }
 
+__device__ __forceinline__ void st_cluster_u32(uint32_t cluster_addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
+}
+
 // One arrival on an mbarrier given by its shared::cluster address (this CTA's or the peer's). Default
 // semantics (release at CTA scope): a cluster-scope release makes the arriving thread wait for all of its earlier
 // global stores, which the callers here neither need nor can afford; what they hand over lives in tensor memory
