@@ -23,6 +23,8 @@
 // (Smaller shares, taken over by CTAs that are done early, were slower: each costs a start and a part.)
 // That kernel also adds up the keys' attention weights where asked: the first one leaves the logits (4 bytes per head and
 // key against 512 per key), from which p = 2^(logit - LSE) follows once the LSE is known.
+#include <algorithm>
+
 #include "sequences.cuh"
 #include "softmax_pipeline.cuh"
 
@@ -437,23 +439,27 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 }
 
 // ------------------------------------------------------------------------------------------
-// The parts of split sequences together, and the keys' weights. Blocks [0, heads_q) of a sequence finish one query head each;
-// with weights, the others take kMassKeys keys of one key-value head each.
+// The parts of split sequences together, and the keys' weights. Of a sequence's blocks the first ones finish some query heads
+// each; with weights, the others take every so many keys of one key-value head each. How many heads and keys go by the number of
+// blocks that makes (launch): each block begins with a chain of loads, so a few hundred are enough.
 // ------------------------------------------------------------------------------------------
 constexpr int kJoinThreads = 128;
+static_assert(kJoinThreads == kHeadDim, "a thread to a number of the output");
 constexpr int kJoinBatch = 8;   // parts that a warp reads at once
 constexpr int kMassKeys = 4 * kJoinThreads;
+constexpr int kJoinBlocks = 592;
 constexpr int kMassHeads = 8;   // whose logits a thread has in flight
 
 template <class Type, int kHeads, bool kMass>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p, int blocks_per_seq, int mass_blocks) {
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p, int head_blocks, int mass_blocks) {
   __shared__ float2 warp_ml[kJoinThreads / 32];
   __shared__ float4 warp_o[kJoinThreads / 32][32];
   extern __shared__ float lse_of[];   // weights: base-2 LSE of the group's query heads
   wait_for_previous_kernel();
   const CacheView& c = p.cache;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int seq = blockIdx.x / blocks_per_seq, what = blockIdx.x % blocks_per_seq;
+  const int blocks_per_seq = head_blocks + c.heads_kv * mass_blocks;
+  const int seq = blockIdx.x / blocks_per_seq, what = blockIdx.x - seq * blocks_per_seq;
   const int heads_q = c.heads_kv * p.group;
   const int head_chunks = (p.group + kHeads - 1) / kHeads, rows = c.heads_kv * head_chunks;
   const int first = __ldcg(p.prefix + seq), n_units = __ldcg(p.prefix + seq + 1) - first;
@@ -466,110 +472,89 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p,
     return make_int2(unit0 / share, (unit0 + n_units - 1) / share);
   };
   auto slot_of = [&](int cta, int2 ctas) -> int64_t { return 2 * cta + (cta == ctas.x ? 1 : 0); };
-  if (what < heads_q) {
-    const int head = what, in_chunk = head % p.group % kHeads;
-    uint16_t* o = p.o + seq * p.o_seq + head * p.o_head;
-    if (n_units == 0) {
-      if (tid < kHeadDim) o[tid] = 0;
-      if (p.lse != nullptr && tid == 0) p.lse[static_cast<int64_t>(seq) * heads_q + head] = -INFINITY;
-      return;
-    }
-    const int2 ctas = ctas_of(head);
-    if (ctas.x == ctas.y) return;   // finished already
-    // Warps take the parts in turn, eight at a time, a lane four numbers of the output: all loads of a batch at once.
-    const int parts = ctas.y - ctas.x + 1;
-    float m = -INFINITY, l = 0.f;
-    float4 o4 = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i0 = warp; i0 < parts; i0 += kJoinBatch * kJoinThreads / 32) {
-      float2 ml[kJoinBatch];
-      float4 x[kJoinBatch];
-      float top = m;
+  if (what < head_blocks) {
+    for (int head = what; head < heads_q; head += head_blocks) {
+      const int in_chunk = head % p.group % kHeads;
+      uint16_t* o = p.o + seq * p.o_seq + head * p.o_head;
+      if (n_units == 0) {
+        if (tid < kHeadDim) o[tid] = 0;
+        if (p.lse != nullptr && tid == 0) p.lse[static_cast<int64_t>(seq) * heads_q + head] = -INFINITY;
+        continue;
+      }
+      const int2 ctas = ctas_of(head);
+      if (ctas.x == ctas.y) continue;   // finished already
+      // Warps take the parts in turn, eight at a time, a lane four numbers of the output: all loads of a batch at once.
+      const int parts = ctas.y - ctas.x + 1;
+      float m = -INFINITY, l = 0.f;
+      float4 o4 = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i0 = warp; i0 < parts; i0 += kJoinBatch * kJoinThreads / 32) {
+        float2 ml[kJoinBatch];
+        float4 x[kJoinBatch];
+        float top = m;
 #pragma unroll
-      for (int j = 0; j < kJoinBatch; ++j) {
-        const int i = i0 + j * kJoinThreads / 32;
-        ml[j] = make_float2(-INFINITY, 0.f);
-        x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (i < parts) {
-          const int64_t at = slot_of(ctas.x + i, ctas) * kHeads + in_chunk;
-          ml[j] = __ldcg(p.part_ml + at);
-          x[j] = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * kHeadDim) + lane);
+        for (int j = 0; j < kJoinBatch; ++j) {
+          const int i = i0 + j * kJoinThreads / 32;
+          ml[j] = make_float2(-INFINITY, 0.f);
+          x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (i < parts) {
+            const int64_t at = slot_of(ctas.x + i, ctas) * kHeads + in_chunk;
+            ml[j] = __ldcg(p.part_ml + at);
+            x[j] = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * kHeadDim) + lane);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < kJoinBatch; ++j) top = fmaxf(top, ml[j].x);
+        const float ref = top == -INFINITY ? 0.f : top, a = fast_exp2(m - ref);
+        m = top;
+        l *= a;
+        o4 = make_float4(o4.x * a, o4.y * a, o4.z * a, o4.w * a);
+#pragma unroll
+        for (int j = 0; j < kJoinBatch; ++j) {
+          const float f = fast_exp2(ml[j].x - ref);
+          l += f * ml[j].y;
+          o4 = make_float4(o4.x + f * x[j].x, o4.y + f * x[j].y, o4.z + f * x[j].z, o4.w + f * x[j].w);
         }
       }
+      if (lane == 0) warp_ml[warp] = make_float2(m, l);
+      warp_o[warp][lane] = o4;
+      __syncthreads();
+      float top = warp_ml[0].x;
 #pragma unroll
-      for (int j = 0; j < kJoinBatch; ++j) top = fmaxf(top, ml[j].x);
-      const float ref = top == -INFINITY ? 0.f : top, a = fast_exp2(m - ref);
-      m = top;
-      l *= a;
-      o4 = make_float4(o4.x * a, o4.y * a, o4.z * a, o4.w * a);
+      for (int w = 1; w < kJoinThreads / 32; ++w) top = fmaxf(top, warp_ml[w].x);
+      const float ref = top == -INFINITY ? 0.f : top;
+      float sum_l = 0.f, sum_o = 0.f;
 #pragma unroll
-      for (int j = 0; j < kJoinBatch; ++j) {
-        const float f = fast_exp2(ml[j].x - ref);
-        l += f * ml[j].y;
-        o4 = make_float4(o4.x + f * x[j].x, o4.y + f * x[j].y, o4.z + f * x[j].z, o4.w + f * x[j].w);
+      for (int w = 0; w < kJoinThreads / 32; ++w) {
+        const float f = fast_exp2(warp_ml[w].x - ref);
+        sum_l += f * warp_ml[w].y;
+        sum_o += f * reinterpret_cast<const float*>(warp_o[w])[tid];
       }
+      const float inv = sum_l == 0.f ? 0.f : 1.f / sum_l;
+      o[tid] = static_cast<uint16_t>(Type::pack(sum_o * inv, 0.f) & 0xffffu);
+      if (p.lse != nullptr && tid == 0) p.lse[static_cast<int64_t>(seq) * heads_q + head] = (top + log2f(sum_l)) * 0.69314718055994531f;
+      __syncthreads();   // the next head's shares go to the same places
     }
-    if (lane == 0) warp_ml[warp] = make_float2(m, l);
-    warp_o[warp][lane] = o4;
-    __syncthreads();
-    if (tid >= kHeadDim) return;
-    float top = warp_ml[0].x;
-#pragma unroll
-    for (int w = 1; w < kJoinThreads / 32; ++w) top = fmaxf(top, warp_ml[w].x);
-    const float ref = top == -INFINITY ? 0.f : top;
-    float sum_l = 0.f, sum_o = 0.f;
-#pragma unroll
-    for (int w = 0; w < kJoinThreads / 32; ++w) {
-      const float f = fast_exp2(warp_ml[w].x - ref);
-      sum_l += f * warp_ml[w].y;
-      sum_o += f * reinterpret_cast<const float*>(warp_o[w])[tid];
-    }
-    const float inv = sum_l == 0.f ? 0.f : 1.f / sum_l;
-    o[tid] = static_cast<uint16_t>(Type::pack(sum_o * inv, 0.f) & 0xffffu);
-    if (p.lse != nullptr && tid == 0) p.lse[static_cast<int64_t>(seq) * heads_q + head] = (top + log2f(sum_l)) * 0.69314718055994531f;
     return;
   }
   if constexpr (!kMass) return;
-  // ---- weights of keys [key0, key0 + kMassKeys) of one key-value head
-  const int kv_head = (what - heads_q) / mass_blocks, key0 = (what - heads_q) % mass_blocks * kMassKeys;
+  // ---- weights: keys [first_key, first_key + kMassKeys) of one key-value head, and so on
+  const int kv_head = (what - head_blocks) / mass_blocks, first_key = (what - head_blocks - kv_head * mass_blocks) * kMassKeys;
   const int len = cached_length(c, seq, p.status, 13);
-  if (key0 >= len) return;
+  if (first_key >= len) return;
   // The first heads' logits are on their way while the heads' LSE is worked out. (A key whose page is missing has -inf there.)
   const int64_t row = static_cast<int64_t>(seq) * c.heads_kv + kv_head;
   const int64_t room = static_cast<int64_t>(c.max_pages) << c.page_shift;
   const float* logits = p.logits + row * p.group * room;
   // four consecutive keys to a thread (rows of logits are whole numbers of 64 bytes)
-  const int j = key0 + 4 * tid;
-  const float* at = logits + j;
-  float4 x[kMassHeads], sum = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto load = [&](int h0) {
+  float4 x[kMassHeads];
+  auto load = [&](int j, int h0) {
 #pragma unroll
     for (int h = 0; h < kMassHeads; ++h) {
       x[h] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (h0 + h < p.group && j < len) x[h] = __ldcg(reinterpret_cast<const float4*>(at + (h0 + h) * room));
+      if (h0 + h < p.group && j < len) x[h] = __ldcg(reinterpret_cast<const float4*>(logits + (h0 + h) * room + j));
     }
   };
-  auto add = [&](float4 v, float lse2) {
-    sum.x += fast_exp2(v.x - lse2);
-    sum.y += fast_exp2(v.y - lse2);
-    sum.z += fast_exp2(v.z - lse2);
-    sum.w += fast_exp2(v.w - lse2);
-  };
-  const float* had = p.mass_in != nullptr ? p.mass_in + row * p.mass_capacity + j : nullptr;
-  float* to = p.mass_out + row * p.mass_capacity + j;
-  const bool vector = j + 4 <= len && p.mass_capacity % 4 == 0 &&
-                      ((reinterpret_cast<uintptr_t>(p.mass_in) | reinterpret_cast<uintptr_t>(p.mass_out)) & 15) == 0;
-  float4 before = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (had != nullptr) {
-    if (vector) {
-      before = __ldcg(reinterpret_cast<const float4*>(had));
-    } else {
-      if (j < len) before.x = __ldcg(had);
-      if (j + 1 < len) before.y = __ldcg(had + 1);
-      if (j + 2 < len) before.z = __ldcg(had + 2);
-      if (j + 3 < len) before.w = __ldcg(had + 3);
-    }
-  }
-  load(0);
+  load(first_key + 4 * tid, 0);
   for (int h = warp; h < p.group; h += kJoinThreads / 32) {
     const int head = kv_head * p.group + h;
     const int2 ctas = ctas_of(head);
@@ -596,23 +581,44 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p,
     if (lane == 0) lse_of[h] = lse2 == -INFINITY ? 0.f : lse2;   // (no key at all: 2^(-inf - 0) = 0)
   }
   __syncthreads();
+  const float* mass_in = p.mass_in != nullptr ? p.mass_in + row * p.mass_capacity : nullptr;
+  float* mass_out = p.mass_out + row * p.mass_capacity;
+  const bool aligned = p.mass_capacity % 4 == 0 && ((reinterpret_cast<uintptr_t>(p.mass_in) | reinterpret_cast<uintptr_t>(p.mass_out)) & 15) == 0;
+  for (int j = first_key + 4 * tid; j - 4 * tid < len; j += mass_blocks * kMassKeys) {
+    const bool vector = aligned && j + 4 <= len;
+    float4 before = make_float4(0.f, 0.f, 0.f, 0.f), sum = before;
+    if (mass_in != nullptr) {
+      if (vector) {
+        before = __ldcg(reinterpret_cast<const float4*>(mass_in + j));
+      } else {
+        if (j < len) before.x = __ldcg(mass_in + j);
+        if (j + 1 < len) before.y = __ldcg(mass_in + j + 1);
+        if (j + 2 < len) before.z = __ldcg(mass_in + j + 2);
+        if (j + 3 < len) before.w = __ldcg(mass_in + j + 3);
+      }
+    }
+    for (int h0 = 0; h0 < p.group; h0 += kMassHeads) {
+      if (h0 > 0) load(j, h0);
 #pragma unroll
-  for (int h = 0; h < kMassHeads; ++h)
-    if (h < p.group) add(x[h], lse_of[h]);
-  for (int h0 = kMassHeads; h0 < p.group; h0 += kMassHeads) {
-    load(h0);
-#pragma unroll
-    for (int h = 0; h < kMassHeads; ++h)
-      if (h0 + h < p.group) add(x[h], lse_of[h0 + h]);
-  }
-  // (the last keys' neighbours in the row of logits may hold anything: they are not stored)
-  if (vector) {
-    *reinterpret_cast<float4*>(to) = make_float4(before.x + sum.x, before.y + sum.y, before.z + sum.z, before.w + sum.w);
-  } else {
-    if (j < len) to[0] = before.x + sum.x;
-    if (j + 1 < len) to[1] = before.y + sum.y;
-    if (j + 2 < len) to[2] = before.z + sum.z;
-    if (j + 3 < len) to[3] = before.w + sum.w;
+      for (int h = 0; h < kMassHeads; ++h)
+        if (h0 + h < p.group) {
+          const float lse2 = lse_of[h0 + h];
+          sum.x += fast_exp2(x[h].x - lse2);
+          sum.y += fast_exp2(x[h].y - lse2);
+          sum.z += fast_exp2(x[h].z - lse2);
+          sum.w += fast_exp2(x[h].w - lse2);
+        }
+    }
+    load(j + mass_blocks * kMassKeys, 0);
+    // (the last keys' neighbours in the row of logits may hold anything: they are not stored)
+    if (vector) {
+      *reinterpret_cast<float4*>(mass_out + j) = make_float4(before.x + sum.x, before.y + sum.y, before.z + sum.z, before.w + sum.w);
+    } else {
+      if (j < len) mass_out[j] = before.x + sum.x;
+      if (j + 1 < len) mass_out[j + 1] = before.y + sum.y;
+      if (j + 2 < len) mass_out[j + 2] = before.z + sum.z;
+      if (j + 3 < len) mass_out[j + 3] = before.w + sum.w;
+    }
   }
 }
 
@@ -627,16 +633,18 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const PagedPara
   if (e != cudaSuccess) return e;
   e = launch_overlapped(kernel, p.ctas, p.ctas, kThreads, smem, stream, tk, tv, p);
   if (e != cudaSuccess) return e;
-  const int room = p.cache.max_pages << p.cache.page_shift;
-  const int mass_blocks = p.mass_out != nullptr ? (room + kMassKeys - 1) / kMassKeys : 0;
-  const int blocks_per_seq = p.cache.heads_kv * (p.group + mass_blocks);
-  const long long blocks = static_cast<long long>(blocks_per_seq) * p.cache.batch;
+  const int heads_q = p.cache.heads_kv * p.group, rows = p.cache.batch * p.cache.heads_kv;
+  const int chunks = ((p.cache.max_pages << p.cache.page_shift) + kMassKeys - 1) / kMassKeys;
+  // about kJoinBlocks blocks for heads, and as many for weights, where there are more heads and keys than that
+  const int head_blocks = std::max(1, std::min(heads_q, kJoinBlocks / p.cache.batch));
+  const int mass_blocks = mass ? std::max(1, std::min(chunks, kJoinBlocks / rows)) : 0;
+  const long long blocks = static_cast<long long>(head_blocks + p.cache.heads_kv * mass_blocks) * p.cache.batch;
   // The joining kernel is overlapped with a main kernel that leaves SMs free. Where that fills the device, the next call's
   // main kernel, overlapped in its turn, would find SMs with the joining CTAs still on them and be placed unevenly (24 x 7000
   // keys x 32 heads, calls back to back: 508 us against 417).
   const long long room_for = full ? 0 : blocks;
-  return mass ? launch_overlapped(join_kernel<Type, kHeads, true>, blocks, room_for, kJoinThreads, p.group * sizeof(float), stream, p, blocks_per_seq, mass_blocks)
-              : launch_overlapped(join_kernel<Type, kHeads, false>, blocks, room_for, kJoinThreads, 0, stream, p, blocks_per_seq, 0);
+  return mass ? launch_overlapped(join_kernel<Type, kHeads, true>, blocks, room_for, kJoinThreads, p.group * sizeof(float), stream, p, head_blocks, mass_blocks)
+              : launch_overlapped(join_kernel<Type, kHeads, false>, blocks, room_for, kJoinThreads, 0, stream, p, head_blocks, 0);
 }
 
 int heads_at_once(int group) { return group <= 8 ? 8 : 16; }
