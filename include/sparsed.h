@@ -373,9 +373,10 @@ sparsed_status sparsed_attn_paged(const sparsed_cache *cache, int32_t heads_q, c
  * the others, the keep - recent with the largest mass (ties, +0 and -0 among them, to the lower position; NaN ranks lowest).
  * Different heads keep different keys of a sequence. `to` has the batch, heads and type of `from`; its pages (of any
  * supported size, of the same pool or another) must not be pages that `from` reads, and its seq_lens, which the call writes,
- * not those of `from`. keep <= to->max_pages * to->page_size, 0 <= recent <= keep, keep >= 1.
+ * not those of `from`. keep >= 1, 0 <= recent <= keep, and `to` has room (max_pages * page_size) for as many keys as `keep`
+ * and the room of `from` allow: most = min(keep, from's max_pages * page_size).
  * mass: device fp32 [batch, heads_kv, mass_capacity], mass_capacity >= from's max_pages * page_size. mass_out: device fp32
- * [batch, heads_kv, mass_out_capacity], mass_out_capacity >= keep: the kept keys' mass, then zeros to the row's end.
+ * [batch, heads_kv, mass_out_capacity], mass_out_capacity >= most: the kept keys' mass, then zeros to the row's end.
  * kept: device int32 [batch, heads_kv, keep]: the kept positions, ascending, -1 behind the last.
  * A kept key whose page does not exist comes over as zeros; one whose new page does not exist is dropped (status 5).
  * Workspace: sparsed_evict_workspace_bytes(from) bytes.

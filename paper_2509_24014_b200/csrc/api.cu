@@ -1120,9 +1120,11 @@ extern "C" sparsed_status sparsed_cache_evict(const sparsed_cache* from, const f
   if (from->seq_lens == to->seq_lens) return SPARSED_ERR_INVALID_ARG;
   if (mass == nullptr || mass_out == nullptr || kept == nullptr || mass == mass_out) return SPARSED_ERR_INVALID_ARG;
   if (keep < 1 || recent < 0 || recent > keep) return SPARSED_ERR_INVALID_ARG;
-  if (keep > static_cast<int64_t>(to->max_pages) * to->page_size) return SPARSED_ERR_INVALID_ARG;
-  if (mass_capacity < static_cast<int64_t>(from->max_pages) * from->page_size || mass_out_capacity < keep)
-    return SPARSED_ERR_INVALID_ARG;
+  // a row has no more keys than its cache has places, whatever `keep` allows (and the places are few enough for 32 bits)
+  const int64_t room = static_cast<int64_t>(from->max_pages) * from->page_size, most = keep < room ? keep : room;
+  if (most > static_cast<int64_t>(to->max_pages) * to->page_size) return SPARSED_ERR_INVALID_ARG;
+  if (mass_capacity < room || mass_out_capacity < most) return SPARSED_ERR_INVALID_ARG;
+  if (keep > (INT32_MAX >> 1)) return SPARSED_ERR_UNSUPPORTED;   // as the places of a cache
   if (static_cast<int64_t>(from->batch) * from->heads_kv * (keep / 32 + 1ll) > INT32_MAX) return SPARSED_ERR_UNSUPPORTED;
   if (!aligned4(mass) || !aligned4(mass_out) || !aligned4(kept)) return SPARSED_ERR_ALIGNMENT;
   if ((st = check_ws(ws, ws_bytes, SPARSED_STATUS_BYTES)) != SPARSED_OK) return st;

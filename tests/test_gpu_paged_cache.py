@@ -352,6 +352,32 @@ def test_evict_within_one_pool():
     assert new_lens.tolist() == [70]
 
 
+@pytest.mark.parametrize("keep,recent", [(33, 0), (40, 40), (5000, 1), (100000, 99999)])
+def test_evict_with_nothing_to_evict(keep, recent):
+    """More may stay than there is room for: all keys move, to as many places as the cache itself has."""
+    lens, gen = [5, 32, 0, 17], su.generator(keep)
+    k, v, table = su.paged_pool(lens, 16, 2, torch.bfloat16, gen)
+    assert table.shape[1] * 16 == 32
+    mass = torch.rand(4, 2, 32, generator=gen, device="cuda")
+    new_k, new_v = torch.zeros_like(k), torch.zeros_like(v)
+    new_lens, kept = i32([-1] * 4), torch.zeros(4, 2, keep, dtype=torch.int32, device="cuda")
+    new_mass = torch.full((4, 2, 32), -1.0, device="cuda")
+    new_table = i32([[2 * b, 2 * b + 1] for b in range(4)])
+    if new_k.shape[0] < 8:
+        new_k, new_v = (torch.zeros(8, *k.shape[1:], dtype=k.dtype, device="cuda") for _ in "kv")
+    ws = sd.new_workspace(256, "cuda")
+    sd.sparsed_cache_evict(sd.make_cache(k, v, table, i32(lens)), mass, keep, recent, sd.make_cache(new_k, new_v, new_table, new_lens),
+                           new_mass, kept, ws)
+    assert su.status(ws)[0] == 0 and new_lens.tolist() == lens
+    for b, n in enumerate(lens):
+        for h in range(2):
+            assert kept[b, h, :n].tolist() == list(range(n)) and (kept[b, h, n:] == -1).all()
+            assert torch.equal(new_mass[b, h, :n], mass[b, h, :n]) and (new_mass[b, h, n:] == 0).all()
+        for j in range(n):
+            assert torch.equal(new_k[2 * b + j // 16, j % 16], k[int(table[b, j // 16]), j % 16])
+            assert torch.equal(new_v[2 * b + j // 16, j % 16], v[int(table[b, j // 16]), j % 16])
+
+
 def test_evict_pages_that_do_not_exist():
     lens, gen = [100], su.generator(4)
     k, v, table = su.paged_pool(lens, 16, 1, torch.bfloat16, gen)

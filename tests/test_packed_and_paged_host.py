@@ -146,9 +146,14 @@ def test_evict_refusals(lib):
     assert call_evict(lib, to=cache()) == 1                                           # writes the lengths it reads
     for kw in (dict(batch=2), dict(heads_kv=1), dict(dtype=1)):
         assert call_evict(lib, to=cache(seq_lens=OK + 64, **kw)) == 1, kw
-    for kw in (dict(keep=0), dict(recent=-1), dict(recent=21), dict(keep=65, out_capacity=100), dict(capacity=63),
+    for kw in (dict(keep=0), dict(recent=-1), dict(recent=21), dict(keep=65, out_capacity=63), dict(capacity=63),
                dict(out_capacity=19), dict(mass=None), dict(mass_out=None), dict(kept=None), dict(mass_out=OK)):
         assert call_evict(lib, **kw) == 1, kw
+    small = cache(seq_lens=OK + 64, page_size=16, max_pages=2)                        # 32 places, of `from` 64
+    assert call_evict(lib, to=small, keep=33, out_capacity=100) == 1 and call_evict(lib, to=small, keep=100, out_capacity=100) == 1
+    # as many as `from` has places, however many may stay: the next check, of the masses' alignment, refuses these
+    assert call_evict(lib, keep=65, out_capacity=64, mass=OK + 2) == 3 and call_evict(lib, to=small, keep=32, out_capacity=32, mass=OK + 2) == 3
+    assert call_evict(lib, keep=(1 << 30) + 5, out_capacity=64) == 2
     for kw in (dict(mass=OK + 2), dict(mass_out=OK + 1), dict(kept=OK + 2), dict(ws=OFF)):
         assert call_evict(lib, **kw) == 3, kw
     assert call_evict(lib, nbytes=100) == 4 and call_evict(lib, ws=None) == 4
