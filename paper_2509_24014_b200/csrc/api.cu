@@ -70,6 +70,22 @@ uint32_t tensor_map_slot(const TensorMapKey& k) {
   return static_cast<uint32_t>(h >> 40) % kTensorMapSlots;
 }
 
+// Any map of 16-bit elements with 128-byte swizzle.
+sparsed_status encode_swizzled_map(CUtensorMap* out, const void* base, int rank, const cuuint64_t* dims,
+                                   const cuuint64_t* stride_bytes, const cuuint32_t* box) {
+  EncodeTiledFn enc = encode_tiled_fn();
+  if (enc == nullptr) return cuda_fail(cudaErrorNotSupported);
+  const cuuint32_t elem[5] = {1, 1, 1, 1, 1};
+  CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, static_cast<cuuint32_t>(rank), const_cast<void*>(base), dims,
+                   stride_bytes, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    g_last_cuda_error = static_cast<int32_t>(r);
+    return SPARSED_ERR_CUDA;
+  }
+  return SPARSED_OK;
+}
+
 // bf16 [B,H,L,128] tensor with element strides (batch, head, token); box = 64 x rows, 128B swizzle.
 sparsed_status make_tensor_map(CUtensorMap* out, const void* base, int batch, int heads, int seq_len,
                                const int64_t strides[3], int box_rows) {
@@ -79,73 +95,50 @@ sparsed_status make_tensor_map(CUtensorMap* out, const void* base, int batch, in
     *out = slot.map;
     return SPARSED_OK;
   }
-  EncodeTiledFn enc = encode_tiled_fn();
-  if (enc == nullptr) return cuda_fail(cudaErrorNotSupported);
   cuuint64_t dims[4] = {128, static_cast<cuuint64_t>(seq_len), static_cast<cuuint64_t>(heads),
                         static_cast<cuuint64_t>(batch)};
   cuuint64_t gstrides[3] = {static_cast<cuuint64_t>(strides[2]) * 2, static_cast<cuuint64_t>(strides[1]) * 2,
                             static_cast<cuuint64_t>(strides[0]) * 2};
   cuuint32_t box[4] = {64, static_cast<cuuint32_t>(box_rows), 1, 1};
-  cuuint32_t elem[4] = {1, 1, 1, 1};
-  CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, gstrides, box, elem,
-                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) {
-    g_last_cuda_error = static_cast<int32_t>(r);
-    return SPARSED_ERR_CUDA;
-  }
+  const sparsed_status st = encode_swizzled_map(out, base, 4, dims, gstrides, box);
+  if (st != SPARSED_OK) return st;
   slot.key = key;
   slot.map = *out;
   slot.valid = true;
   return SPARSED_OK;
 }
 
-// Any map of 16-bit elements with 128-byte swizzle, cached like those above under a key of its own kind (box_rows < 0).
-sparsed_status make_swizzled_map(CUtensorMap* out, const TensorMapKey& key, int rank, const cuuint64_t* dims,
-                                 const cuuint64_t* stride_bytes, const cuuint32_t* box) {
-  TensorMapSlot& slot = g_tensor_maps[tensor_map_slot(key)];
-  if (slot.valid && slot.key == key) {
-    *out = slot.map;
-    return SPARSED_OK;
-  }
-  EncodeTiledFn enc = encode_tiled_fn();
-  if (enc == nullptr) return cuda_fail(cudaErrorNotSupported);
-  const cuuint32_t elem[5] = {1, 1, 1, 1, 1};
-  CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, static_cast<cuuint32_t>(rank), const_cast<void*>(key.base), dims,
-                   stride_bytes, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) {
-    g_last_cuda_error = static_cast<int32_t>(r);
-    return SPARSED_ERR_CUDA;
-  }
-  slot.key = key;
-  slot.map = *out;
-  slot.valid = true;
-  return SPARSED_OK;
+// The maps of the packed and paged calls are encoded anew for every call.
+// Packed keys or values, [total, heads, 128] with element strides (token, head), under a batch of one as above; box = 64 x
+// box_rows tokens.
+sparsed_status make_packed_key_map(CUtensorMap* out, const void* base, int total, int heads, const int64_t strides[2], int box_rows) {
+  const cuuint64_t dims[4] = {128, static_cast<cuuint64_t>(total), static_cast<cuuint64_t>(heads), 1};
+  const cuuint64_t token = static_cast<cuuint64_t>(strides[0]) * 2, head = static_cast<cuuint64_t>(strides[1]) * 2;
+  const cuuint64_t stride_bytes[3] = {token, head, token};
+  const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(box_rows), 1, 1};
+  return encode_swizzled_map(out, base, 4, dims, stride_bytes, box);
 }
 
 // One pool of a paged cache, [pages, places, heads, 128] with element strides (page, place, head), as [pages, heads, 2 halves,
 // places, 64]; box = 64 x 16 places x both halves.
 sparsed_status make_pool_map(CUtensorMap* out, const void* base, int pages, int places, int heads, int64_t page_stride,
                              int64_t place_stride, int64_t head_stride) {
-  const TensorMapKey key{base, {page_stride, place_stride, head_stride}, pages, heads, places, -1};
   const cuuint64_t dims[5] = {64, static_cast<cuuint64_t>(places), 2, static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(pages)};
   const cuuint64_t strides[4] = {static_cast<cuuint64_t>(place_stride) * 2, 128, static_cast<cuuint64_t>(head_stride) * 2,
                                  static_cast<cuuint64_t>(page_stride) * 2};
   const cuuint32_t box[5] = {64, 16, 2, 1, 1};
-  return make_swizzled_map(out, key, 5, dims, strides, box);
+  return encode_swizzled_map(out, base, 5, dims, strides, box);
 }
 
 // Packed queries, [total, heads, 128] with element strides (token, head), as [key-value heads, total, heads of a group, 128];
 // box = 64 x `pack` heads x `tokens`.
 sparsed_status make_packed_query_map(CUtensorMap* out, const void* base, int total, int heads_kv, int group, int64_t token_stride,
                                      int64_t head_stride, int pack, int tokens) {
-  const TensorMapKey key{base, {token_stride, head_stride, group}, heads_kv, pack, total, -2};
   const cuuint64_t dims[4] = {128, static_cast<cuuint64_t>(group), static_cast<cuuint64_t>(total), static_cast<cuuint64_t>(heads_kv)};
   const cuuint64_t strides[3] = {static_cast<cuuint64_t>(head_stride) * 2, static_cast<cuuint64_t>(token_stride) * 2,
                                  static_cast<cuuint64_t>(head_stride) * 2 * group};
   const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(pack), static_cast<cuuint32_t>(tokens), 1};
-  return make_swizzled_map(out, key, 4, dims, strides, box);
+  return encode_swizzled_map(out, base, 4, dims, strides, box);
 }
 
 struct Resolved {
@@ -966,14 +959,13 @@ extern "C" sparsed_status sparsed_attn_packed(const sparsed_packed* shape, const
   if (nothing) return SPARSED_OK;
   if ((st = check_arch()) != SPARSED_OK) return st;
   CUtensorMap tq, tk, tv;
-  const int64_t k3[3] = {ks[0], ks[1], ks[0]}, v3[3] = {vs[0], vs[1], vs[0]};
   if ((st = make_packed_query_map(&tq, q, shape->total_q, shape->heads_kv, p.group, qs[0], qs[1], p.pack, p.tile_tokens)) != SPARSED_OK)
     return st;
   if (no_keys) {
     tk = tv = tq;   // (nothing is loaded through them)
   } else {
-    if ((st = make_tensor_map(&tk, k, 1, shape->heads_kv, shape->total_k, k3, pair ? 32 : 64)) != SPARSED_OK) return st;
-    if ((st = make_tensor_map(&tv, v, 1, shape->heads_kv, shape->total_k, v3, 64)) != SPARSED_OK) return st;
+    if ((st = make_packed_key_map(&tk, k, shape->total_k, shape->heads_kv, ks, pair ? 32 : 64)) != SPARSED_OK) return st;
+    if ((st = make_packed_key_map(&tv, v, shape->total_k, shape->heads_kv, vs, 64)) != SPARSED_OK) return st;
   }
   p.cu_q = cu_q;
   p.cu_k = cu_k;
@@ -1036,7 +1028,8 @@ static sparsed_status check_paged_sizes(const sparsed_cache* cache, int32_t head
   if (st != SPARSED_OK) return st;
   if (heads_q < 1 || heads_q % cache->heads_kv != 0) return SPARSED_ERR_INVALID_ARG;
   const int64_t keys = static_cast<int64_t>(cache->max_pages) * cache->page_size;
-  if (static_cast<int64_t>(cache->batch) * heads_q * (keys / 64 + 1) > INT32_MAX) return SPARSED_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(cache->batch) * heads_q * (keys / 64 + 1) > INT32_MAX / 2) return SPARSED_ERR_UNSUPPORTED;
+  if (heads_q / cache->heads_kv > 4096) return SPARSED_ERR_UNSUPPORTED;   // (their LSE lie in shared memory, 16 KB)
   return SPARSED_OK;
 }
 
