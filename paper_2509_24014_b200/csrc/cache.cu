@@ -13,7 +13,9 @@ constexpr int kRowChunks = 16;   // 16-byte chunks of a head's 128 numbers
 
 // ------------------------------------------------------------------------------------------
 // New tokens into the cache. A warp moves one token (all heads of K and V), four 512-byte pieces of each at a time; the first
-// ones are on their way while it looks for the token's sequence and place.
+// ones are on their way while it looks for the token's sequence and place. Nothing is computed or rounded. Bound by HBM: prompts
+// of 330 MB of keys and values, read once and written once, in 107 us (6.2 TB/s); one token each of 64 sequences, which is the
+// chain offsets - length - page alone, in 2.3.
 // ------------------------------------------------------------------------------------------
 constexpr int kWriteWarps = 8;
 
@@ -63,38 +65,49 @@ __global__ void __launch_bounds__(32 * kWriteWarps) cache_write_kernel(const Cac
 
 // ------------------------------------------------------------------------------------------
 // Eviction, first half: which keys stay. A cluster of CTAs ranks one row (sequence, key-value head), each CTA a run of its
-// candidates (all but the `recent` last keys): radix selection of the (keep - recent)-th largest mass, 11 + 11 + 10 bits. Each
-// CTA counts its keys in a histogram of its own; then each adds up a slice of the bins over the cluster and scans it, and all
-// find the bin from the slices' totals (every CTA adding up every bin for itself took 2.5 us a step for a cluster of eight, 0.5
-// this way). At the end every warp counts and writes out its share in order. Bound by the latency of these steps.
+// candidates (all but the `recent` last keys): radix selection of the (keep - recent)-th largest mass, 11 + 11 + 10 bits of a key
+// that orders like the float, ended early once all of the bin that holds it stay. Each CTA counts its keys in a histogram of its
+// own; then each adds up a slice of the bins over the cluster and scans it, and all find the bin from the slices' totals (every CTA
+// adding up every bin for itself took 2.5 us a step for a cluster of eight, 0.5 this way). At the end every warp counts and writes
+// out its share in order. Nothing is rounded: masses are compared and copied.
+//
+// Bound by the latency of these steps, and with 1024 threads by their instructions: of 8.3 us for 3000 candidates in one CTA (with
+// cold caches) the loads take 2.7, a step 0.5 for counting, 0.25 for adding up and 0.2 for the bin, the writing 2.2; of 18 us for
+// 13,000 in each of four CTAs 5, 3 and 7.
 // ------------------------------------------------------------------------------------------
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectWarps = kSelectThreads / 32;
 constexpr int kMostRanks = 8;    // CTAs to a row
 constexpr int kBins = 2048;
+constexpr int kScanThreads = 256;   // that add up and scan the bins (with all 1024 the instructions of it took twice as long)
+constexpr int kLoadBatch = 4;    // weights that a thread has on their way when a CTA reads its run
+constexpr int kWriteBatch = 8;   // times 32 keys whose weights a warp has on their way when it writes out its share
 constexpr uint32_t kZeroKey = 0x80000000u;   // ordered_key(0)
 constexpr int kCachedKeys = 24 * 1024;   // of a CTA's run, held in shared memory (96 KB) as ordered keys
 
 struct EvictSmem {
+  alignas(16) uint32_t keys[kCachedKeys];
   int hist[kBins];
-  int count[kBins], above[kBins];   // of this CTA's slice of the bins: keys in each over the cluster, and in the slice's bins above it
+  int2 slice[kBins];       // of this CTA's slice of the bins: keys in each over the cluster, and in the slice's bins above it
   int slice_total;
-  int warp_sum[kSelectWarps];
-  int found_bin, found_above;
+  int warp_sum[kScanThreads / 32];
+  int found_bin, found_above, found_count;
   int keys_above[kSelectWarps], keys_equal[kSelectWarps];   // above / equal to the threshold in each warp's share
   int cta_above, cta_equal;
-  uint32_t keys[kCachedKeys];
+  int zeros;               // keys of weight zero in this CTA's run
 };
 
-__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const EvictParams p) {
+// ranks: CTAs to a row (1, 2, 4 or 8).
+template <int ranks>
+__global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const EvictParams p) {
   namespace cg = cooperative_groups;
   extern __shared__ __align__(16) uint8_t smem_raw[];
   EvictSmem& sm = *reinterpret_cast<EvictSmem*>(smem_raw);
   wait_for_previous_kernel();
   cg::cluster_group cluster = cg::this_cluster();
-  const int ranks = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
+  const int rank = ranks == 1 ? 0 : static_cast<int>(cluster.block_rank());
   auto sync_row = [&]() {
-    if (ranks == 1) __syncthreads();
+    if constexpr (ranks == 1) __syncthreads();
     else cluster.sync();
   };
   const int row = blockIdx.x / ranks;   // sequence * heads_kv + head
@@ -118,101 +131,169 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
     return;
   }
   const int candidates = len - p.recent, need = p.keep - p.recent;
-  for (int j = me; j < p.recent; j += all) {
-    kept[need + j] = candidates + j;
-    mass_out[need + j] = __ldcg(mass + candidates + j);
+  const float recent_mass = me < p.recent ? __ldcg(mass + candidates + me) : 0.f;
+  auto keep_recent = [&]() {
+    if (me < p.recent) {
+      kept[need + me] = candidates + me;
+      mass_out[need + me] = recent_mass;
+    }
+    for (int j = me + all; j < p.recent; j += all) {
+      kept[need + j] = candidates + j;
+      mass_out[need + j] = __ldcg(mass + candidates + j);
+    }
+  };
+  if (need == 0) {
+    keep_recent();
+    return;
   }
-  if (need == 0) return;
-  // this CTA's run of candidates, in whole warps' shares
-  const int share = (candidates + ranks * kSelectWarps - 1) / (ranks * kSelectWarps);   // candidates per warp
+  // this CTA's run of candidates, in whole warps' shares of whole fours
+  const int share = (candidates + ranks * kSelectWarps * 4 - 1) / (ranks * kSelectWarps * 4) * 4;   // candidates per warp
   const int run0 = min(rank * kSelectWarps * share, candidates), run1 = min((rank + 1) * kSelectWarps * share, candidates);
   const int run = run1 - run0;
   const int cached = min(run, kCachedKeys);
-#pragma unroll 4
-  for (int i = tid; i < cached; i += kSelectThreads) sm.keys[i] = ordered_key(__ldcg(mass + run0 + i));
-  auto key_at = [&](int i) -> uint32_t { return i < kCachedKeys ? sm.keys[i] : ordered_key(__ldcg(mass + run0 + i)); };
+  if (tid == 0) sm.zeros = 0;
+  for (int i = tid; i < kBins; i += kSelectThreads) sm.hist[i] = 0;
+  __syncthreads();
+  // Weights of exactly zero (keys that no query has looked at) are often most of a row: they are counted here once, and not by
+  // thousands of additions to one place of every histogram.
+  int zeros = 0;
+  for (int i0 = tid; i0 < cached; i0 += kLoadBatch * kSelectThreads) {
+    float x[kLoadBatch];
+#pragma unroll
+    for (int j = 0; j < kLoadBatch; ++j) x[j] = i0 + j * kSelectThreads < cached ? __ldcg(mass + run0 + i0 + j * kSelectThreads) : 1.f;
+#pragma unroll
+    for (int j = 0; j < kLoadBatch; ++j) {
+      const uint32_t key = ordered_key(x[j]);
+      if (i0 + j * kSelectThreads < cached) sm.keys[i0 + j * kSelectThreads] = key;
+      zeros += key == kZeroKey;
+    }
+  }
+  keep_recent();
+  for (int i = cached + tid; i < run; i += kSelectThreads) zeros += ordered_key(__ldcg(mass + run0 + i)) == kZeroKey;
+  zeros = __reduce_add_sync(0xffffffffu, zeros);
+  if (lane == 0 && zeros > 0) atomicAdd(&sm.zeros, zeros);
+  // keys i to i + 3 of the run (i a multiple of 4); how many of them there are
+  auto keys_at = [&](int i, uint32_t (&key)[4]) -> int {
+    if (i + 4 <= cached) {
+      const uint4 x = *reinterpret_cast<const uint4*>(sm.keys + i);
+      key[0] = x.x, key[1] = x.y, key[2] = x.z, key[3] = x.w;
+      return 4;
+    }
+    const int n = min(run - i, 4);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) key[x] = x >= n ? 0u : (i + x < cached ? sm.keys[i + x] : ordered_key(__ldcg(mass + run0 + i + x)));
+    return n;
+  };
+  __syncthreads();
   // ---- the threshold -----------------------------------------------------------------------
   uint32_t prefix = 0u;
   int left = need;          // of the keys that agree with `prefix` in the bits decided so far
-  const int slice = kBins / ranks;   // bins that each CTA adds up: 2048, 1024, 512 or 256
+  constexpr int kSlice = kBins / ranks, kPerThread = kSlice / kScanThreads;   // bins that each CTA, and each thread, adds up
   for (int step = 0; step < 3; ++step) {
-    const int shift = step == 0 ? 21 : (step == 1 ? 10 : 0);
-    const int bins = step == 2 ? 1024 : kBins;
-    for (int i = tid; i < kBins; i += kSelectThreads) sm.hist[i] = 0;
-    __syncthreads();
-    // Weights of exactly zero (keys that no query has looked at) are often most of a row: they are counted in registers, and
-    // not by thousands of additions to one place.
-    int zeros = 0;
-    for (int i = tid; i < run; i += kSelectThreads) {
-      const uint32_t key = key_at(i);
-      const bool in = step == 0 || ((key ^ prefix) >> (shift + (step == 1 ? 11 : 10))) == 0u;
-      if (in && key == kZeroKey) ++zeros;
-      if (in && key != kZeroKey) atomicAdd(&sm.hist[(key >> shift) & (bins - 1)], 1);
+    const int shift = step == 0 ? 21 : (step == 1 ? 10 : 0), decided = shift + (step == 2 ? 10 : 11);
+    const uint32_t bins = step == 2 ? 1024u : kBins;
+    for (int i = 4 * tid; i < run; i += 4 * kSelectThreads) {
+      uint32_t key[4];
+      const int n = keys_at(i, key);
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        if (x < n && key[x] != kZeroKey && (step == 0 || (key[x] ^ prefix) >> decided == 0u)) atomicAdd(&sm.hist[(key[x] >> shift) & (bins - 1u)], 1);
     }
-    zeros = __reduce_add_sync(0xffffffffu, zeros);
-    if (lane == 0 && zeros > 0) atomicAdd(&sm.hist[(kZeroKey >> shift) & (bins - 1)], zeros);
+    if (tid == 0 && (step == 0 || (kZeroKey ^ prefix) >> decided == 0u)) atomicAdd(&sm.hist[(kZeroKey >> shift) & (bins - 1u)], sm.zeros);
     sync_row();
-    // This CTA's slice: the bins from rank * slice on, the highest first, two to a thread (one, where a slice has fewer).
-    const int per_thread = slice > kSelectThreads ? 2 : 1;
-    int hi = 0, lo = 0;
-    const int hi_bin = rank * slice + slice - 1 - per_thread * tid;   // (and the one below it)
-    const bool mine = per_thread * tid < slice;
-    if (mine) {
+    // This CTA's slice: the bins from rank * kSlice on, the highest first, a few to a thread.
+    int in[kPerThread], sum = 0;
+    const int first_bin = rank * kSlice + kSlice - 1 - kPerThread * tid;   // (and those below it)
+    if (tid < kScanThreads) {
 #pragma unroll
-      for (int r = 0; r < kMostRanks; ++r)
-        if (r < ranks) hi += *cluster.map_shared_rank(&sm.hist[hi_bin], r);
-      if (per_thread == 2) lo = sm.hist[hi_bin - 1];   // (one CTA to the row)
-    }
-    int sum = hi + lo;
+      for (int x = 0; x < kPerThread; ++x) in[x] = 0;
 #pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-      const int other = __shfl_up_sync(0xffffffffu, sum, d);
-      if (lane >= d) sum += other;
-    }
-    if (lane == 31) sm.warp_sum[warp] = sum;
-    __syncthreads();
-    sum += __reduce_add_sync(0xffffffffu, lane < warp ? sm.warp_sum[lane] : 0);
-    if (mine) {
-      const int at = hi_bin - rank * slice;
-      sm.count[at] = hi;
-      sm.above[at] = sum - lo - hi;
-      if (per_thread == 2) {
-        sm.count[at - 1] = lo;
-        sm.above[at - 1] = sum - lo;
+      for (int r = 0; r < ranks; ++r)
+#pragma unroll
+        for (int x = 0; x < kPerThread; ++x) in[x] += ranks == 1 ? sm.hist[first_bin - x] : *cluster.map_shared_rank(&sm.hist[first_bin - x], r);
+#pragma unroll
+      for (int x = 0; x < kPerThread; ++x) sum += in[x];
+      const int own = sum;
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) {
+        const int other = __shfl_up_sync(0xffffffffu, sum, d);
+        if (lane >= d) sum += other;
       }
+      if (lane == 31) sm.warp_sum[warp] = sum;
+      named_barrier_sync(1, kScanThreads);
+      sum += __reduce_add_sync(0xffffffffu, lane < warp ? sm.warp_sum[lane] : 0) - own;   // in the slice's bins above
     }
-    if (tid == kSelectThreads - 1) sm.slice_total = sum;
-    sync_row();
-    // The slice in which the count from the top passes `left`, then the bin: every CTA looks for itself.
-    const int total = lane < ranks ? *cluster.map_shared_rank(&sm.slice_total, ranks - 1 - lane) : 0;   // lane 0: the highest slice
-    int upto = total;
+    if constexpr (ranks == 1) {
+      if (tid < kScanThreads) {
 #pragma unroll
-    for (int d = 1; d < kMostRanks; d *= 2) {
-      const int other = __shfl_up_sync(0xffffffffu, upto, d);
-      if (lane >= d) upto += other;
-    }
-    const int at_lane = __ffs(__ballot_sync(0xffffffffu, lane < ranks && upto >= left)) - 1;   // (the lowest reaches it at last)
-    const int owner = ranks - 1 - at_lane, before = __shfl_sync(0xffffffffu, upto - total, at_lane);
-    for (int i = tid; i < slice; i += kSelectThreads) {
-      const int above = before + *cluster.map_shared_rank(&sm.above[i], owner), in = *cluster.map_shared_rank(&sm.count[i], owner);
-      if (above < left && above + in >= left) {
-        sm.found_bin = owner * slice + i;
-        sm.found_above = above;
+        for (int x = 0; x < kPerThread; ++x) {
+          if (sum < left && sum + in[x] >= left) {
+            sm.found_bin = first_bin - x;
+            sm.found_above = sum;
+            sm.found_count = in[x];
+          }
+          sum += in[x];
+        }
       }
+      __syncthreads();
+      for (int i = tid; i < kBins; i += kSelectThreads) sm.hist[i] = 0;
+      __syncthreads();
+    } else {
+      if (tid < kScanThreads) {
+#pragma unroll
+        for (int x = 0; x < kPerThread; ++x) {
+          sm.slice[first_bin - rank * kSlice - x] = make_int2(in[x], sum);
+          sum += in[x];
+        }
+        if (tid == kScanThreads - 1) sm.slice_total = sum;
+      }
+      sync_row();
+      for (int i = tid; i < kBins; i += kSelectThreads) sm.hist[i] = 0;   // (all have read it)
+      // The slice in which the count from the top passes `left`, then the bin: every CTA looks for itself.
+      if (tid < kScanThreads) {
+        const int total = lane < ranks ? *cluster.map_shared_rank(&sm.slice_total, ranks - 1 - lane) : 0;   // lane 0: the highest slice
+        int upto = total;
+#pragma unroll
+        for (int d = 1; d < ranks; d *= 2) {
+          const int other = __shfl_up_sync(0xffffffffu, upto, d);
+          if (lane >= d) upto += other;
+        }
+        const int at_lane = __ffs(__ballot_sync(0xffffffffu, lane < ranks && upto >= left)) - 1;   // (the lowest reaches it at last)
+        const int owner = ranks - 1 - at_lane, before = __shfl_sync(0xffffffffu, upto - total, at_lane);
+        int2 bin[kPerThread];
+#pragma unroll
+        for (int x = 0; x < kPerThread; ++x) bin[x] = *cluster.map_shared_rank(&sm.slice[x * kScanThreads + tid], owner);
+#pragma unroll
+        for (int x = 0; x < kPerThread; ++x)
+          if (before + bin[x].y < left && before + bin[x].y + bin[x].x >= left) {
+            sm.found_bin = owner * kSlice + x * kScanThreads + tid;
+            sm.found_above = before + bin[x].y;
+            sm.found_count = bin[x].x;
+          }
+      }
+      __syncthreads();
+      // (the slices are read by other CTAs until they come to the next step's first barrier, and written behind it)
     }
-    __syncthreads();
     prefix |= static_cast<uint32_t>(sm.found_bin) << shift;
     left -= sm.found_above;
-    // (count and above are read by other CTAs until they come to the next step's first barrier, and written behind it)
+    if (left == sm.found_count && prefix != 0u) {   // the whole bin stays: the lower bits need not be known
+      --prefix;
+      left = 0;
+      break;
+    }
   }
   // Kept: keys above `prefix`, and the first `left` of those equal to it.
   // ---- where each warp's share goes ----------------------------------------------------------
   const int my0 = min(warp * share, run), my1 = min(my0 + share, run);
   int above = 0, equal = 0;
-  for (int i = my0 + lane; i < my1; i += 32) {
-    const uint32_t key = key_at(i);
-    above += key > prefix;
-    equal += key == prefix;
+  for (int i = my0 + 4 * lane; i < my1; i += 128) {
+    uint32_t key[4];
+    const int n = min(keys_at(i, key), my1 - i);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      above += x < n && key[x] > prefix;
+      equal += x < n && key[x] == prefix;
+    }
   }
   above = __reduce_add_sync(0xffffffffu, above);
   equal = __reduce_add_sync(0xffffffffu, equal);
@@ -230,31 +311,42 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
   }
   sync_row();
   // in the shares before this warp's: those of CTAs before (a lane each) and of warps before
-  int above_before = lane < rank ? *cluster.map_shared_rank(&sm.cta_above, lane) : 0;
-  int equal_before = lane < rank ? *cluster.map_shared_rank(&sm.cta_equal, lane) : 0;
+  int above_before = 0, equal_before = 0;
+  if (ranks > 1 && lane < rank) {
+    above_before = *cluster.map_shared_rank(&sm.cta_above, lane);
+    equal_before = *cluster.map_shared_rank(&sm.cta_equal, lane);
+  }
   above_before = __reduce_add_sync(0xffffffffu, above_before + (lane < warp ? sm.keys_above[lane] : 0));
   equal_before = __reduce_add_sync(0xffffffffu, equal_before + (lane < warp ? sm.keys_equal[lane] : 0));
-  for (int i0 = my0; i0 < my1; i0 += 32) {
-    const int i = i0 + lane;
-    const uint32_t key = i < my1 ? key_at(i) : 0u;
-    const bool is_above = i < my1 && key > prefix, is_equal = i < my1 && key == prefix;
-    const uint32_t lower = (1u << lane) - 1u;
-    const uint32_t a = __ballot_sync(0xffffffffu, is_above), e = __ballot_sync(0xffffffffu, is_equal);
-    const int my_equal = equal_before + __popc(e & lower);
-    if (is_above || (is_equal && my_equal < left)) {
-      const int at = above_before + __popc(a & lower) + min(my_equal, left);
-      kept[at] = run0 + i;
-      mass_out[at] = __ldcg(mass + run0 + i);
+  const uint32_t lower = (1u << lane) - 1u;
+  for (int i0 = my0; i0 < my1; i0 += 32 * kWriteBatch) {
+    float weight[kWriteBatch];   // (as it is: a key does not tell NaNs apart, nor zeros)
+#pragma unroll
+    for (int x = 0; x < kWriteBatch; ++x) weight[x] = i0 + 32 * x + lane < my1 ? __ldcg(mass + run0 + i0 + 32 * x + lane) : 0.f;
+#pragma unroll
+    for (int x = 0; x < kWriteBatch; ++x) {
+      if (i0 + 32 * x >= my1) break;
+      const int i = i0 + 32 * x + lane;
+      const uint32_t key = i >= my1 ? 0u : (i < cached ? sm.keys[i] : ordered_key(weight[x]));
+      const bool is_above = i < my1 && key > prefix, is_equal = i < my1 && key == prefix;
+      const uint32_t a = __ballot_sync(0xffffffffu, is_above), e = __ballot_sync(0xffffffffu, is_equal);
+      const int my_equal = equal_before + __popc(e & lower);
+      if (is_above || (is_equal && my_equal < left)) {
+        const int at = above_before + __popc(a & lower) + min(my_equal, left);
+        kept[at] = run0 + i;
+        mass_out[at] = weight[x];
+      }
+      above_before += __popc(a);
+      equal_before += __popc(e);
     }
-    above_before += __popc(a);
-    equal_before += __popc(e);
   }
-  sync_row();   // no CTA leaves while another may still read its counts
+  if constexpr (ranks > 1) sync_row();   // no CTA leaves while another may still read its counts
 }
 
 // ------------------------------------------------------------------------------------------
 // Eviction, second half: the kept rows of K and V to their new pages. A warp moves 32 keys of a row: each lane looks up one
 // key's place and its new one, then sixteen lanes at a time move a key's 256 bytes, four keys of K and V in flight per lane.
+// Bound by HBM: whole calls move 2 x 16384 keys x 8 heads in 69.5 us (18 of them the selection, then 5.3 TB/s, read and written).
 // ------------------------------------------------------------------------------------------
 constexpr int kMoveThreads = 128;
 
@@ -312,15 +404,20 @@ cudaError_t launch_cache_write(const CacheWriteParams& p, cudaStream_t stream) {
 cudaError_t launch_cache_evict(const EvictParams& p, cudaStream_t stream) {
   const int rows = p.from.batch * p.from.heads_kv;
   const int smem = static_cast<int>(sizeof(EvictSmem));
-  static SmemLimit limit;
-  cudaError_t e = ensure_dynamic_smem(evict_select_kernel, smem, limit);
-  if (e != cudaSuccess) return e;
   // Several CTAs to a row that is long enough to be shared, as long as they take no more than 64 SMs: a CTA needs an SM for
-  // itself and a cluster the SMs of one part of the device, so more would not run at the same time (16 rows of 52k in clusters
-  // of 8: two rounds, the call 89.5 us; of 4: 73.3; of 2: 93.9; one CTA to a row: 140. 32 rows of 4k: 32.6, 30.2, 29.9, 29.1).
+  // itself and a cluster the SMs of one part of the device, so more would not run at the same time. The whole call, us: 16 rows of
+  // 52k in clusters of 8 (two rounds) 74.1, of 4 69.5, of 2 87.0, one CTA to a row 120; 8 rows of 128k, 8 49.9, 4 49.9, 2 74.5,
+  // one 123; 4 rows of 32k, 8 19.9, 4 20.2, 2 21.5. Of short rows a cluster's barriers and remote reads cost more than it gains:
+  // 32 rows of up to 4k, one CTA 22.2, two 28.1; 16 rows of 8000, one 17.5, two 19.6, four 19.1; 8 of 16000, two 20.7, four 18.9.
   const int room = p.from.max_pages << p.from.page_shift;
   int ranks = 1;
   while (ranks < kMostRanks && rows * ranks * 2 <= 64 && room / (2 * ranks) >= 2048) ranks *= 2;
+  static SmemLimit limits[4];
+  const int which = ranks == 1 ? 0 : (ranks == 2 ? 1 : (ranks == 4 ? 2 : 3));
+  constexpr decltype(&evict_select_kernel<1>) kernels[4] = {evict_select_kernel<1>, evict_select_kernel<2>, evict_select_kernel<4>,
+                                                            evict_select_kernel<8>};
+  cudaError_t e = ensure_dynamic_smem(kernels[which], smem, limits[which]);
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(rows * ranks));
   cfg.blockDim = dim3(kSelectThreads);
@@ -334,7 +431,7 @@ cudaError_t launch_cache_evict(const EvictParams& p, cudaStream_t stream) {
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  e = cudaLaunchKernelEx(&cfg, evict_select_kernel, p);
+  e = cudaLaunchKernelEx(&cfg, kernels[which], p);
   if (e == cudaSuccess) {
     cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>((static_cast<int64_t>((p.keep + 31) / 32) * rows + kMoveThreads / 32 - 1) / (kMoveThreads / 32)));
