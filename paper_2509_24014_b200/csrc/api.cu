@@ -1078,7 +1078,7 @@ extern "C" sparsed_status sparsed_attn_paged(const sparsed_cache* cache, int32_t
   p.mass_out = mass_out_or_null;
   p.mass_capacity = mass_capacity;
   p.group = group;
-  p.ctas = 0;
+  p.ctas = p.fills = 0;   // (launch_attn_paged)
   p.prefix = reinterpret_cast<int32_t*>(base + at.prefix);
   p.lse2 = reinterpret_cast<float*>(base + at.lse2);
   p.part_ml = reinterpret_cast<float2*>(base + at.part_ml);

@@ -23,6 +23,14 @@
 // (Smaller shares, taken over by CTAs that are done early, were slower: each costs a start and a part.)
 // That kernel also adds up the keys' attention weights where asked: the first one leaves the logits (4 bytes per head and
 // key against 512 per key), from which p = 2^(logit - LSE) follows once the LSE is known.
+//
+// Roundings: logits, sums, O and weights are fp32 throughout. P goes to the matrix instructions in the cache's 16-bit type, the
+// sum of a softmax takes it unrounded: half a step of P, 2^-9 of a weight in bf16 and 2^-12 in fp16, with either sign, averages
+// out over the keys (errors against 64 bits 2.3e-3 of O's size in bf16, most of it O's own rounding, 2.9e-4 in fp16).
+//
+// Measured (caches cold): 24 x 6000-8192 keys x 32 heads 416 us, 6.7 TB/s; 131072 x 8 heads 90, 5.9; 48 x 300-8000 x 4 heads
+// 53, 4.4 (with weights 57); one sequence of 1500 keys x 4 heads 7.5 in a graph. The shorter ones are bound by what comes before
+// and after the stream of keys: lengths - page - first tiles, about 3 us, and the joining kernel, 4 to 8.
 #include <algorithm>
 
 #include "sequences.cuh"
@@ -93,7 +101,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   constexpr int kNT = kHeads / 8;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   PagedSmem<kHeads>& sm = *reinterpret_cast<PagedSmem<kHeads>*>(smem_raw);
-  wait_for_previous_kernel();
+  wait_for_previous_kernel(!p.fills);
   if ((smem_u32(smem_raw) & 1023u) != 0u) {
     if (threadIdx.x == 0) record_status(p.status, 2, 5);
     return;
@@ -381,6 +389,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     unit += tile1 - tile0;
     buf ^= 1;
     if (unit < unit1) begin_segment();
+    else if (p.fills) next_kernel_may_start();
     // o[n][j]: d = 8 * spread + j (0, 1) and 64 + 8 * spread + j (2, 3) of heads 2t and 2t + 1 of n-tile n
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
@@ -455,7 +464,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p,
   __shared__ float2 warp_ml[kJoinThreads / 32];
   __shared__ float4 warp_o[kJoinThreads / 32][32];
   extern __shared__ float lse_of[];   // weights: base-2 LSE of the group's query heads
-  wait_for_previous_kernel();
+  wait_for_previous_kernel(!p.fills);
   const CacheView& c = p.cache;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int blocks_per_seq = head_blocks + c.heads_kv * mass_blocks;
@@ -546,8 +555,24 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p,
   const int64_t room = static_cast<int64_t>(c.max_pages) << c.page_shift;
   const float* logits = p.logits + row * p.group * room;
   // four consecutive keys to a thread (rows of logits are whole numbers of 64 bytes)
-  float4 x[kMassHeads];
+  const float* mass_in = p.mass_in != nullptr ? p.mass_in + row * p.mass_capacity : nullptr;
+  float* mass_out = p.mass_out + row * p.mass_capacity;
+  const bool aligned = p.mass_capacity % 4 == 0 && ((reinterpret_cast<uintptr_t>(p.mass_in) | reinterpret_cast<uintptr_t>(p.mass_out)) & 15) == 0;
+  float4 x[kMassHeads], before;
   auto load = [&](int j, int h0) {
+    if (h0 == 0) {
+      before = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (mass_in != nullptr) {
+        if (aligned && j + 4 <= len) {
+          before = __ldcg(reinterpret_cast<const float4*>(mass_in + j));
+        } else {
+          if (j < len) before.x = __ldcg(mass_in + j);
+          if (j + 1 < len) before.y = __ldcg(mass_in + j + 1);
+          if (j + 2 < len) before.z = __ldcg(mass_in + j + 2);
+          if (j + 3 < len) before.w = __ldcg(mass_in + j + 3);
+        }
+      }
+    }
 #pragma unroll
     for (int h = 0; h < kMassHeads; ++h) {
       x[h] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -581,22 +606,8 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p,
     if (lane == 0) lse_of[h] = lse2 == -INFINITY ? 0.f : lse2;   // (no key at all: 2^(-inf - 0) = 0)
   }
   __syncthreads();
-  const float* mass_in = p.mass_in != nullptr ? p.mass_in + row * p.mass_capacity : nullptr;
-  float* mass_out = p.mass_out + row * p.mass_capacity;
-  const bool aligned = p.mass_capacity % 4 == 0 && ((reinterpret_cast<uintptr_t>(p.mass_in) | reinterpret_cast<uintptr_t>(p.mass_out)) & 15) == 0;
   for (int j = first_key + 4 * tid; j - 4 * tid < len; j += mass_blocks * kMassKeys) {
-    const bool vector = aligned && j + 4 <= len;
-    float4 before = make_float4(0.f, 0.f, 0.f, 0.f), sum = before;
-    if (mass_in != nullptr) {
-      if (vector) {
-        before = __ldcg(reinterpret_cast<const float4*>(mass_in + j));
-      } else {
-        if (j < len) before.x = __ldcg(mass_in + j);
-        if (j + 1 < len) before.y = __ldcg(mass_in + j + 1);
-        if (j + 2 < len) before.z = __ldcg(mass_in + j + 2);
-        if (j + 3 < len) before.w = __ldcg(mass_in + j + 3);
-      }
-    }
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int h0 = 0; h0 < p.group; h0 += kMassHeads) {
       if (h0 > 0) load(j, h0);
 #pragma unroll
@@ -609,21 +620,27 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p,
           sum.w += fast_exp2(x[h].w - lse2);
         }
     }
+    sum = make_float4(before.x + sum.x, before.y + sum.y, before.z + sum.z, before.w + sum.w);
     load(j + mass_blocks * kMassKeys, 0);
     // (the last keys' neighbours in the row of logits may hold anything: they are not stored)
-    if (vector) {
-      *reinterpret_cast<float4*>(mass_out + j) = make_float4(before.x + sum.x, before.y + sum.y, before.z + sum.z, before.w + sum.w);
+    if (aligned && j + 4 <= len) {
+      *reinterpret_cast<float4*>(mass_out + j) = sum;
     } else {
-      if (j < len) mass_out[j] = before.x + sum.x;
-      if (j + 1 < len) mass_out[j + 1] = before.y + sum.y;
-      if (j + 2 < len) mass_out[j + 2] = before.z + sum.z;
-      if (j + 3 < len) mass_out[j + 3] = before.w + sum.w;
+      if (j < len) mass_out[j] = sum.x;
+      if (j + 1 < len) mass_out[j + 1] = sum.y;
+      if (j + 2 < len) mass_out[j + 2] = sum.z;
+      if (j + 3 < len) mass_out[j + 3] = sum.w;
     }
   }
 }
 
+// The joining kernel is always started early. Where the main kernel fills the device (p.fills), that is when its CTAs come to their
+// last segment's end, and the joining kernel in its turn does not let the next one start before it is done: the next call's main
+// kernel would find SMs with joining CTAs still on them and be placed unevenly (24 x 7000 keys x 32 heads, calls back to back: 508
+// us against 417). Against a joining kernel that is started when the main one is done: 48 conversations of 300 to 8000 keys x 4
+// heads 56.0 -> 52.6 us, with weights 59.9 -> 56.8, 128k x 8 heads 92.7 -> 90.5.
 template <class Type, int kHeads>
-cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const PagedParams& p, bool full, cudaStream_t stream) {
+cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const PagedParams& p, cudaStream_t stream) {
   const bool mass = p.mass_out != nullptr;
   auto kernel = mass ? attn_paged_kernel<Type, kHeads, true> : attn_paged_kernel<Type, kHeads, false>;
   const int smem = static_cast<int>(sizeof(PagedSmem<kHeads>));
@@ -639,12 +656,8 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const PagedPara
   const int head_blocks = std::max(1, std::min(heads_q, kJoinBlocks / p.cache.batch));
   const int mass_blocks = mass ? std::max(1, std::min(chunks, kJoinBlocks / rows)) : 0;
   const long long blocks = static_cast<long long>(head_blocks + p.cache.heads_kv * mass_blocks) * p.cache.batch;
-  // The joining kernel is overlapped with a main kernel that leaves SMs free. Where that fills the device, the next call's
-  // main kernel, overlapped in its turn, would find SMs with the joining CTAs still on them and be placed unevenly (24 x 7000
-  // keys x 32 heads, calls back to back: 508 us against 417).
-  const long long room_for = full ? 0 : blocks;
-  return mass ? launch_overlapped(join_kernel<Type, kHeads, true>, blocks, room_for, kJoinThreads, p.group * sizeof(float), stream, p, head_blocks, mass_blocks)
-              : launch_overlapped(join_kernel<Type, kHeads, false>, blocks, room_for, kJoinThreads, 0, stream, p, head_blocks, 0);
+  return mass ? launch_overlapped(join_kernel<Type, kHeads, true>, blocks, blocks, kJoinThreads, p.group * sizeof(float), stream, p, head_blocks, mass_blocks)
+              : launch_overlapped(join_kernel<Type, kHeads, false>, blocks, blocks, kJoinThreads, 0, stream, p, head_blocks, 0);
 }
 
 int heads_at_once(int group) { return group <= 8 ? 8 : 16; }
@@ -675,10 +688,10 @@ cudaError_t launch_attn_paged(const CUtensorMap& tk, const CUtensorMap& tv, Page
   const int heads = heads_at_once(p.group);
   const int fit = sms * ctas_per_sm(heads);
   const int most = paged_max_ctas(p.cache.batch, p.cache.heads_kv, p.group, p.cache.max_pages, 1 << p.cache.page_shift);
-  const bool full = fit <= most;
-  p.ctas = full ? fit : most;
-  if (heads == 8) return fp16 ? launch<Fp16Type, 8>(tk, tv, p, full, stream) : launch<Bf16Type, 8>(tk, tv, p, full, stream);
-  return fp16 ? launch<Fp16Type, 16>(tk, tv, p, full, stream) : launch<Bf16Type, 16>(tk, tv, p, full, stream);
+  p.fills = fit <= most;
+  p.ctas = p.fills ? fit : most;
+  if (heads == 8) return fp16 ? launch<Fp16Type, 8>(tk, tv, p, stream) : launch<Bf16Type, 8>(tk, tv, p, stream);
+  return fp16 ? launch<Fp16Type, 16>(tk, tv, p, stream) : launch<Bf16Type, 16>(tk, tv, p, stream);
 }
 
 }  // namespace sparsed

@@ -71,6 +71,7 @@ struct PagedParams {
   int group;               // query heads per key-value head
   float scale_log2;
   int ctas;                // of the main kernel
+  int fills;               // whether these fill the device
   // scratch
   int32_t* prefix;         // [batch + 1] key tiles of the sequences before, for one head
   float* lse2;             // [batch, heads_q] base-2 LSE of sequences that one CTA has done by itself

@@ -118,9 +118,10 @@ __device__ __forceinline__ bool mbar_wait2(uint64_t* bar_a, uint32_t parity_a, u
 // writes are visible; only then is the next kernel allowed to start, so that at most two kernels of a stream
 // overlap. Data that an earlier kernel may have written is read with TMA, __ldcg, __ldcs or plain loads, not __ldg.
 // ----------------------------------------------------------------------------
-__device__ __forceinline__ void wait_for_previous_kernel() {
+__device__ __forceinline__ void next_kernel_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous_kernel(bool next_may_start = true) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (next_may_start) next_kernel_may_start();
 }
 
 // ----------------------------------------------------------------------------
