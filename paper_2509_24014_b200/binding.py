@@ -419,6 +419,7 @@ _DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_FP16}
 _PACKED_RECORD = struct.Struct("@8i8qf%dx" % (ctypes.sizeof(Packed) - struct.calcsize("@8i8qf")))
 _TWO_STRIDES = struct.Struct("@2q")
 _int32, _fp32 = torch.int32, torch.float32
+_BROADCAST = "a broadcast tensor (strides of zero): its rows have to exist"
 _ELSEWHERE = "all tensors of a call must be on the same device"
 
 
@@ -439,7 +440,10 @@ def _call(device: int, what: str, function, *args) -> None:
 def _row_strides(shape, strides) -> Tuple[int, int]:
     """Strides (row, head) of a [rows, heads, 128] tensor. (A dimension of one or no rows may have any stride.)"""
     head = strides[1] if shape[1] > 1 else shape[2]
-    return (strides[0] if shape[0] > 1 else max(shape[1] * shape[2], head)), head
+    row = strides[0] if shape[0] > 1 else max(shape[1] * shape[2], head)
+    if not (row and head):   # (the library takes strides of zero for "contiguous")
+        raise ValueError(_BROADCAST)
+    return row, head
 
 
 def _offsets_ok(t: torch.Tensor, entries: int) -> bool:
@@ -492,7 +496,14 @@ def make_cache(k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, seq_l
 
     def strides(t):   # a dimension of one place may have any stride
         head = t.stride(2) if t.shape[2] > 1 else t.shape[3]
-        return (t.stride(0) if t.shape[0] > 1 else max(t.stride(1) * t.shape[1], head * t.shape[2])), t.stride(1), head
+        place = t.stride(1) if t.shape[1] > 1 else head * t.shape[2]
+        page = t.stride(0) if t.shape[0] > 1 else max(place * t.shape[1], head * t.shape[2])
+        if not (page and place and head):
+            raise ValueError(_BROADCAST)
+        return page, place, head
+
+    if page_table.shape[0] > 1 and page_table.stride(0) == 0:
+        raise ValueError(_BROADCAST)
 
     c = Cache(k.data_ptr(), v.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(),
               page_table.stride(0) if page_table.shape[0] > 1 else 0, (ctypes.c_int64 * 3)(*strides(k)),

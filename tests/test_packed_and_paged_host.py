@@ -203,6 +203,67 @@ def su_cu(n):
     return torch.zeros(n + 1, dtype=torch.int32)
 
 
+def test_broadcast_tensors_are_refused():
+    """Strides of zero mean contiguous to the library: a tensor that has them would be read beyond its end."""
+    cu, ws = torch.tensor([0, 4], dtype=torch.int32), torch.zeros(256, dtype=torch.uint8)
+    q, one = torch.zeros(4, 2, 128, dtype=torch.bfloat16), torch.zeros(1, 1, 128, dtype=torch.bfloat16)
+    for wide in (one.expand(4, 2, 128), torch.zeros(4, 1, 128, dtype=torch.bfloat16).expand(4, 2, 128),
+                 torch.zeros(1, 2, 128, dtype=torch.bfloat16).expand(4, 2, 128)):
+        for args in ((wide, q, q, q), (q, wide, q, q), (q, q, wide, q), (q, q, q, wide)):
+            with pytest.raises(ValueError, match="broadcast"):
+                sd.sparsed_attn_packed(*args, cu, cu, ws)
+    pool, lens = torch.zeros(5, 16, 2, 128, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    table = torch.zeros(3, 4, dtype=torch.int32)
+    for args in ((torch.zeros(1, 1, 1, 128, dtype=torch.bfloat16).expand(5, 16, 2, 128), pool, table, lens),
+                 (pool, pool[:1].expand(5, 16, 2, 128), table, lens), (pool, pool[:, :, :1].expand(5, 16, 2, 128), table, lens),
+                 (pool, pool, table[:1].expand(3, 4), lens)):
+        with pytest.raises(ValueError, match="broadcast"):
+            sd.make_cache(*args)
+    cache = sd.make_cache(pool, pool, table, lens)
+    q3 = torch.zeros(3, 2, 128, dtype=torch.bfloat16)
+    for args in ((one.expand(3, 2, 128), q3), (q3, one.expand(3, 2, 128))):
+        with pytest.raises(ValueError, match="broadcast"):
+            sd.sparsed_attn_paged(args[0], cache, args[1], ws)
+        with pytest.raises(ValueError, match="broadcast"):
+            sd.sparsed_cache_write(cache, *args, torch.zeros(4, dtype=torch.int32), ws)
+    # one row of everything may have any stride
+    c = sd.make_cache(pool[:1].expand(1, 16, 2, 128), pool[:1], table[:1].expand(1, 4), lens[:1])
+    assert (c.table_stride, tuple(c.k_strides)) == (0, (16 * 2 * 128, 256, 128))
+
+
+def test_the_current_device_is_the_tensors(monkeypatch):
+    """A call whose tensors are on another device than the current one runs with theirs current, on their stream."""
+    entered, called = [], []
+
+    class FakeDevice:
+        def __init__(self, device):
+            self.device = device
+
+        def __enter__(self):
+            entered.append(self.device)
+
+        def __exit__(self, *error):
+            entered.append("left")
+
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 1000 + device, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch.cuda, "device", FakeDevice)
+
+    def function(*args):
+        called.append((args, list(entered)))
+        return 0
+
+    binding._call(1, "call", function, "a")
+    assert called == [(("a", 1001), [1])] and entered == [1, "left"]
+    binding._call(0, "call", function, "b")
+    assert called[1] == (("b", 1000), [1, "left"]) and len(entered) == 2
+    with pytest.raises(sd.SparsedError):
+        binding._call(1, "call", lambda *a: 1)
+    assert entered[-1] == "left"
+    with pytest.raises(ValueError, match="CUDA"):
+        binding._call(-1, "call", function)
+
+
 def test_struct_layouts_match_header():
     assert ctypes.sizeof(binding.Packed) == 8 * 4 + 8 * 8 + 8
     assert ctypes.sizeof(binding.Cache) == 4 * 8 + 8 + 6 * 8 + 7 * 4 + 4
