@@ -1022,6 +1022,12 @@ extern "C" sparsed_status sparsed_cache_write(const sparsed_cache* cache, const 
   return e == cudaSuccess ? SPARSED_OK : cuda_fail(e);
 }
 
+// Whether two arrays of 4-byte elements share any.
+static bool overlap(const void* a, int64_t n_a, const void* b, int64_t n_b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y ? y - x < static_cast<uintptr_t>(n_a) * 4 : x - y < static_cast<uintptr_t>(n_b) * 4;
+}
+
 // The sizes of a paged call: query heads, and units of work that are counted in 32 bits.
 static sparsed_status check_paged_sizes(const sparsed_cache* cache, int32_t heads_q) {
   sparsed_status st = check_cache_sizes(cache);
@@ -1110,17 +1116,19 @@ extern "C" sparsed_status sparsed_cache_evict(const sparsed_cache* from, const f
   if (st != SPARSED_OK) return st;
   if ((st = check_cache(to, &p.to)) != SPARSED_OK) return st;
   if (from->batch != to->batch || from->heads_kv != to->heads_kv || from->dtype != to->dtype) return SPARSED_ERR_INVALID_ARG;
-  if (from->seq_lens == to->seq_lens) return SPARSED_ERR_INVALID_ARG;
-  if (mass == nullptr || mass_out == nullptr || kept == nullptr || mass == mass_out) return SPARSED_ERR_INVALID_ARG;
+  if (overlap(from->seq_lens, from->batch, to->seq_lens, to->batch)) return SPARSED_ERR_INVALID_ARG;   // (read by many CTAs while it is written)
+  if (mass == nullptr || mass_out == nullptr || kept == nullptr) return SPARSED_ERR_INVALID_ARG;
   if (keep < 1 || recent < 0 || recent > keep) return SPARSED_ERR_INVALID_ARG;
   // a row has no more keys than its cache has places, whatever `keep` allows (and the places are few enough for 32 bits)
   const int64_t room = static_cast<int64_t>(from->max_pages) * from->page_size, most = keep < room ? keep : room;
   if (most > static_cast<int64_t>(to->max_pages) * to->page_size) return SPARSED_ERR_INVALID_ARG;
   if (mass_capacity < room || mass_out_capacity < most) return SPARSED_ERR_INVALID_ARG;
   if (keep > (INT32_MAX >> 1)) return SPARSED_ERR_UNSUPPORTED;   // as the places of a cache
-  if (static_cast<int64_t>(from->batch) * from->heads_kv * (keep / 32 + 1ll) > INT32_MAX) return SPARSED_ERR_UNSUPPORTED;
+  const int64_t rows = static_cast<int64_t>(from->batch) * from->heads_kv;
+  if (rows * (keep / 32 + 1ll) > INT32_MAX / 2) return SPARSED_ERR_UNSUPPORTED;
   if (!aligned4(mass) || !aligned4(mass_out) || !aligned4(kept)) return SPARSED_ERR_ALIGNMENT;
   if ((st = check_ws(ws, ws_bytes, SPARSED_STATUS_BYTES)) != SPARSED_OK) return st;
+  if (overlap(mass, rows * mass_capacity, mass_out, rows * mass_out_capacity)) return SPARSED_ERR_INVALID_ARG;
   if ((st = check_arch()) != SPARSED_OK) return st;
   p.mass = mass;
   p.mass_out = mass_out;

@@ -386,7 +386,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     const bool whole = tile0 == 0 && tile1 == n_units;
     const int slot = 2 * static_cast<int>(blockIdx.x) + (tile0 == 0 ? 1 : 0);
     const int done_seq = seq, done_head0 = head0, done_heads = heads;
-    unit += tile1 - tile0;
+    unit += max(tile1 - tile0, 1);   // (less than one only where the lengths change under the call)
     buf ^= 1;
     if (unit < unit1) begin_segment();
     else if (p.fills) next_kernel_may_start();
@@ -548,7 +548,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p,
   if constexpr (!kMass) return;
   // ---- weights: keys [first_key, first_key + kMassKeys) of one key-value head, and so on
   const int kv_head = (what - head_blocks) / mass_blocks, first_key = (what - head_blocks - kv_head * mass_blocks) * kMassKeys;
-  const int len = cached_length(c, seq, p.status, 13);
+  const int len = min(cached_length(c, seq, p.status, 13), n_units * kUnit);   // (n_units * kUnit: lengths that change under the call)
   if (first_key >= len) return;
   // The first heads' logits are on their way while the heads' LSE is worked out. (A key whose page is missing has -inf there.)
   const int64_t row = static_cast<int64_t>(seq) * c.heads_kv + kv_head;

@@ -217,3 +217,22 @@ def test_offsets_that_point_nowhere_are_reported_and_not_followed(cu_q, cu_k):
     sd.sparsed_attn_packed(q, k, v, o, cu, cu, ws, causal=True)
     torch.cuda.synchronize()
     assert su.status(ws) == (0, 0)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_offsets_beyond_32_bits(causal):
+    """Rows of q, k, v and o more than 2^32 elements from the start; what lies before belongs to sequences of no keys or queries."""
+    total, heads, n = 1_060_000, 32, 300
+    assert (total - n) * heads * 128 > 1 << 32
+    gen = su.generator(16)
+    q, k, v, o = (torch.empty(total, heads, 128, dtype=torch.bfloat16, device="cuda") for _ in "qkvo")
+    for t in (q, k, v):
+        t[total - n:] = su.rows(n, heads, torch.bfloat16, gen)
+    v[total - 5, 3, 7] = float("inf")
+    cu_q, cu_k = su.offsets([total - n, 0, n]), su.offsets([0, total - n, n])
+    o[:8] = 7.0
+    lse = torch.zeros(heads, total, device="cuda")
+    run(q, k, v, cu_q, cu_k, causal, o=o, lse=lse)
+    want, want_lse = run(*(t[total - n:].clone() for t in (q, k, v)), su.offsets([n]), su.offsets([n]), causal)
+    assert torch.equal(o[total - n:].view(torch.int16), want.view(torch.int16)) and torch.equal(lse[:, total - n:], want_lse)
+    assert (o[:total - n] == 0).all() and (lse[:, :total - n] == -float("inf")).all()

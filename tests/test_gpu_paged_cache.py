@@ -234,6 +234,31 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+def test_written_and_moved_beyond_32_bits():
+    """New tokens into pages at the far end of a pool, and an eviction from there to the far end."""
+    pages, page_size, heads_kv = 16500, 256, 8
+    k = torch.zeros(pages, page_size, heads_kv, 128, dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    gen, ws = su.generator(15), sd.new_workspace(256, "cuda")
+    table, new_table = i32([[pages - 1, pages - 4, 2]]), i32([[pages - 2]])
+    n = i32([600])
+    cache = sd.make_cache(k, v, table, n)
+    k_new, v_new = (su.rows(600, heads_kv, torch.bfloat16, gen) for _ in "kv")
+    sd.sparsed_cache_write(cache, k_new, v_new, i32([0, 600]), ws)
+    for j in (0, 255, 256, 511, 512, 599):
+        assert torch.equal(k[table[0, j // 256], j % 256], k_new[j]) and torch.equal(v[table[0, j // 256], j % 256], v_new[j])
+    assert int((k != 0).any(-1).any(-1).sum()) == 600
+    mass = torch.rand(1, heads_kv, 768, generator=gen, device="cuda")
+    new_lens, new_mass = i32([0]), torch.zeros(1, heads_kv, 256, device="cuda")
+    kept = torch.zeros(1, heads_kv, 100, dtype=torch.int32, device="cuda")
+    sd.sparsed_cache_evict(cache, mass, 100, 10, sd.make_cache(k, v, new_table, new_lens), new_mass, kept, ws)
+    assert su.status(ws) == (0, 0) and new_lens.tolist() == [100]
+    for h in range(heads_kv):
+        stay = orc.kept_positions(mass[0, h].cpu().numpy(), 600, 100, 10)
+        assert kept[0, h].tolist() == list(stay)
+        assert torch.equal(k[pages - 2, :100, h], k_new[stay, h]) and torch.equal(v[pages - 2, :100, h], v_new[stay, h])
+
+
 def test_graph_replays_read_the_lengths_of_the_moment():
     lens, gen = [200, 900], su.generator(13)
     k, v, table = su.paged_pool([1000, 1000], 64, 2, torch.bfloat16, gen)

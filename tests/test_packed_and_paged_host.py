@@ -154,6 +154,11 @@ def test_evict_refusals(lib):
     # as many as `from` has places, however many may stay: the next check, of the masses' alignment, refuses these
     assert call_evict(lib, keep=65, out_capacity=64, mass=OK + 2) == 3 and call_evict(lib, to=small, keep=32, out_capacity=32, mass=OK + 2) == 3
     assert call_evict(lib, keep=(1 << 30) + 5, out_capacity=64) == 2
+    # arrays that the call writes while others of its CTAs read them: lengths (3 of them), masses (3 x 2 rows)
+    for off in (-8, -4, 4, 8):
+        assert call_evict(lib, to=cache(seq_lens=OK + off)) == 1, off
+    for off in (-6 * 20 * 4 + 4, 4, 6 * 64 * 4 - 4):
+        assert call_evict(lib, mass_out=OK + off) == 1, off
     for kw in (dict(mass=OK + 2), dict(mass_out=OK + 1), dict(kept=OK + 2), dict(ws=OFF)):
         assert call_evict(lib, **kw) == 3, kw
     assert call_evict(lib, nbytes=100) == 4 and call_evict(lib, ws=None) == 4
