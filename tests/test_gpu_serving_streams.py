@@ -167,6 +167,24 @@ def test_packed_many_sequences():
     check(q, k, v, lens, lens, True)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+def test_a_sequences_bits_do_not_depend_on_the_batch(causal):
+    lens, gen = [70, 1, 300, 128, 41], su.generator(15)
+    q, k, v = (su.rows(sum(lens), h, torch.bfloat16, gen) for h in (14, 2, 2))
+    at, ws = 0, sd.new_workspace(256, "cuda")
+
+    def call(q, k, v, lens):
+        o = torch.zeros_like(q)
+        sd.sparsed_attn_packed(q, k, v, o, su.offsets(lens), su.offsets(lens), ws, causal=causal)
+        return o
+
+    batch = call(q, k, v, lens)
+    for n in lens:
+        assert torch.equal(call(q[at:at + n], k[at:at + n], v[at:at + n], [n]), batch[at:at + n])
+        at += n
+    assert su.status(ws) == (0, 0)
+
+
 def test_packed_keys_that_are_the_values():
     lens, gen = [70, 300], su.generator(8)
     q, kv = su.rows(370, 8, torch.bfloat16, gen), su.rows(370, 2, torch.bfloat16, gen)
