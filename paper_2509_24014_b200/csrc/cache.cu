@@ -75,34 +75,36 @@ __global__ void __launch_bounds__(32 * kWriteWarps) cache_write_kernel(const Cac
 // cold caches) the loads take 2.7, a step 0.5 for counting, 0.25 for adding up and 0.2 for the bin, the writing 2.2; of 18 us for
 // 13,000 in each of four CTAs 5, 3 and 7.
 // ------------------------------------------------------------------------------------------
-constexpr int kSelectThreads = 1024;
-constexpr int kSelectWarps = kSelectThreads / 32;
 constexpr int kMostRanks = 8;    // CTAs to a row
+constexpr int kShortRow = 2048;  // the most keys of a row that a CTA of 256 threads takes
 constexpr int kBins = 2048;
 constexpr int kScanThreads = 256;   // that add up and scan the bins (with all 1024 the instructions of it took twice as long)
 constexpr int kLoadBatch = 4;    // weights that a thread has on their way when a CTA reads its run
 constexpr int kWriteBatch = 8;   // times 32 keys whose weights a warp has on their way when it writes out its share
 constexpr uint32_t kZeroKey = 0x80000000u;   // ordered_key(0)
-constexpr int kCachedKeys = 24 * 1024;   // of a CTA's run, held in shared memory (96 KB) as ordered keys
+// of a CTA's run, held in shared memory (96 KB, 8 KB) as ordered keys
+__host__ __device__ constexpr int cached_keys(int threads) { return threads == 1024 ? 24 * 1024 : kShortRow; }
 
+template <int ranks, int threads>
 struct EvictSmem {
-  alignas(16) uint32_t keys[kCachedKeys];
+  alignas(16) uint32_t keys[cached_keys(threads)];
   int hist[kBins];
-  int2 slice[kBins];       // of this CTA's slice of the bins: keys in each over the cluster, and in the slice's bins above it
+  int2 slice[ranks > 1 ? kBins / ranks : 1];   // of this CTA's slice of the bins: keys in each over the cluster, and in the slice's bins above it
   int slice_total;
   int warp_sum[kScanThreads / 32];
   int found_bin, found_above, found_count;
-  int keys_above[kSelectWarps], keys_equal[kSelectWarps];   // above / equal to the threshold in each warp's share
+  int keys_above[threads / 32], keys_equal[threads / 32];   // above / equal to the threshold in each warp's share
   int cta_above, cta_equal;
   int zeros;               // keys of weight zero in this CTA's run
 };
 
 // ranks: CTAs to a row (1, 2, 4 or 8).
-template <int ranks>
-__global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const EvictParams p) {
+template <int ranks, int kSelectThreads>
+__global__ void __launch_bounds__(kSelectThreads, 1024 / kSelectThreads) evict_select_kernel(const EvictParams p) {
   namespace cg = cooperative_groups;
+  constexpr int kSelectWarps = kSelectThreads / 32, kCachedKeys = cached_keys(kSelectThreads);
   extern __shared__ __align__(16) uint8_t smem_raw[];
-  EvictSmem& sm = *reinterpret_cast<EvictSmem*>(smem_raw);
+  auto& sm = *reinterpret_cast<EvictSmem<ranks, kSelectThreads>*>(smem_raw);
   wait_for_previous_kernel();
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = ranks == 1 ? 0 : static_cast<int>(cluster.block_rank());
@@ -303,7 +305,8 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const E
   }
   __syncthreads();
   if (warp == 0) {
-    const int a = __reduce_add_sync(0xffffffffu, sm.keys_above[lane]), e = __reduce_add_sync(0xffffffffu, sm.keys_equal[lane]);
+    const int a = __reduce_add_sync(0xffffffffu, lane < kSelectWarps ? sm.keys_above[lane] : 0);
+    const int e = __reduce_add_sync(0xffffffffu, lane < kSelectWarps ? sm.keys_equal[lane] : 0);
     if (lane == 0) {
       sm.cta_above = a;
       sm.cta_equal = e;
@@ -403,7 +406,6 @@ cudaError_t launch_cache_write(const CacheWriteParams& p, cudaStream_t stream) {
 
 cudaError_t launch_cache_evict(const EvictParams& p, cudaStream_t stream) {
   const int rows = p.from.batch * p.from.heads_kv;
-  const int smem = static_cast<int>(sizeof(EvictSmem));
   // Several CTAs to a row that is long enough to be shared, as long as they take no more than 64 SMs: a CTA needs an SM for
   // itself and a cluster the SMs of one part of the device, so more would not run at the same time. The whole call, us: 16 rows of
   // 52k in clusters of 8 (two rounds) 74.1, of 4 69.5, of 2 87.0, one CTA to a row 120; 8 rows of 128k, 8 49.9, 4 49.9, 2 74.5,
@@ -412,16 +414,26 @@ cudaError_t launch_cache_evict(const EvictParams& p, cudaStream_t stream) {
   const int room = p.from.max_pages << p.from.page_shift;
   int ranks = 1;
   while (ranks < kMostRanks && rows * ranks * 2 <= 64 && room / (2 * ranks) >= 2048) ranks *= 2;
-  static SmemLimit limits[4];
-  const int which = ranks == 1 ? 0 : (ranks == 2 ? 1 : (ranks == 4 ? 2 : 3));
-  constexpr decltype(&evict_select_kernel<1>) kernels[4] = {evict_select_kernel<1>, evict_select_kernel<2>, evict_select_kernel<4>,
-                                                            evict_select_kernel<8>};
-  cudaError_t e = ensure_dynamic_smem(kernels[which], smem, limits[which]);
+  // Short rows get CTAs of 256 threads, four to an SM: the call with 1024 | 256 threads, us, 352 rows of up to 59 keys 22.2 | 14.0,
+  // 148 of 1000 23.2 | 20.4, 32 of 1000 12.3 | 11.6, 4 of 1000 10.9 | 10.3, 128 of 2000 22.5 | 19.9; but 32 of 2000 13.3 | 13.7 and
+  // 256 of 4000 41.6 | 43.3.
+  const bool short_rows = room <= (rows > 64 ? kShortRow : kShortRow / 2);
+  struct Variant {
+    void (*kernel)(EvictParams);
+    int threads, smem;
+  };
+  constexpr Variant variants[5] = {{evict_select_kernel<1, 1024>, 1024, sizeof(EvictSmem<1, 1024>)}, {evict_select_kernel<2, 1024>, 1024, sizeof(EvictSmem<2, 1024>)},
+                                   {evict_select_kernel<4, 1024>, 1024, sizeof(EvictSmem<4, 1024>)}, {evict_select_kernel<8, 1024>, 1024, sizeof(EvictSmem<8, 1024>)},
+                                   {evict_select_kernel<1, 256>, 256, sizeof(EvictSmem<1, 256>)}};
+  const int which = ranks > 1 ? (ranks == 2 ? 1 : (ranks == 4 ? 2 : 3)) : (short_rows ? 4 : 0);
+  const Variant& variant = variants[which];
+  static SmemLimit limits[5];
+  cudaError_t e = ensure_dynamic_smem(variant.kernel, variant.smem, limits[which]);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(rows * ranks));
-  cfg.blockDim = dim3(kSelectThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.blockDim = dim3(static_cast<unsigned>(variant.threads));
+  cfg.dynamicSmemBytes = static_cast<size_t>(variant.smem);
   cfg.stream = stream;
   cudaLaunchAttribute attr[2] = {};
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -431,7 +443,7 @@ cudaError_t launch_cache_evict(const EvictParams& p, cudaStream_t stream) {
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  e = cudaLaunchKernelEx(&cfg, kernels[which], p);
+  e = cudaLaunchKernelEx(&cfg, variant.kernel, p);
   if (e == cudaSuccess) {
     cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>((static_cast<int64_t>((p.keep + 31) / 32) * rows + kMoveThreads / 32 - 1) / (kMoveThreads / 32)));

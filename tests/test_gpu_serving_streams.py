@@ -250,9 +250,9 @@ def test_write_wide_rows_and_slices():
     assert torch.equal(k, want_k) and torch.equal(v, want_v)
 
 
-@pytest.mark.parametrize("batch,heads_kv,length", [(1, 1, 100001), (3, 7, 20000), (70, 1, 2100)])
+@pytest.mark.parametrize("batch,heads_kv,length", [(1, 1, 100001), (3, 7, 20000), (70, 1, 2100), (70, 1, 2040), (64, 1, 2040), (2, 1, 1000)])
 def test_evict_is_the_same_again(batch, heads_kv, length):
-    """Rows over one, four and eight CTAs of a cluster: the same places again, whoever runs beside."""
+    """Rows over one, four and eight CTAs of a cluster, and over CTAs of 1024 and 256 threads: the places by the definition."""
     gen = su.generator(14)
     k, v, table = su.paged_pool([length] * batch, 256, heads_kv, torch.bfloat16, gen)
     mass = torch.rand(batch, heads_kv, table.shape[1] * 256, generator=gen, device="cuda").round(decimals=3)
