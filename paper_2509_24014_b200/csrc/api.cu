@@ -1017,6 +1017,7 @@ extern "C" sparsed_status sparsed_cache_write(const sparsed_cache* cache, const 
   p.v_head = vs[1];
   p.cu = cu_new;
   p.total = total_new;
+  p.tokens_at_once = p.tokens_per_warp = 1;
   p.status = static_cast<DeviceStatus*>(ws);
   cudaError_t e = launch_cache_write(p, static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? SPARSED_OK : cuda_fail(e);

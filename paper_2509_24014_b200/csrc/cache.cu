@@ -12,54 +12,68 @@ namespace {
 constexpr int kRowChunks = 16;   // 16-byte chunks of a head's 128 numbers
 
 // ------------------------------------------------------------------------------------------
-// New tokens into the cache. A warp moves one token (all heads of K and V), four 512-byte pieces of each at a time; the first
-// ones are on their way while it looks for the token's sequence and place. Nothing is computed or rounded. Bound by HBM: prompts
-// of 330 MB of keys and values, read once and written once, in 107 us (6.2 TB/s); one token each of 64 sequences, which is the
-// chain offsets - length - page alone, in 2.3.
+// New tokens into the cache. A warp moves a run of tokens (all heads of K and V), four 512-byte pieces of each at a time, of one
+// token or, with few heads, of several; the first ones are on their way while it looks for the first token's sequence and place, and
+// from then on it goes from sequence to sequence by itself. Nothing is computed or rounded. Bound by HBM: prompts of 330 MB of
+// keys and values, read once and written once, in 107 us (6.2 TB/s); one token each of 64 sequences, which is the chain offsets -
+// length - page alone, in 2.3 in a graph.
 // ------------------------------------------------------------------------------------------
 constexpr int kWriteWarps = 8;
+constexpr int kWriteChunks = 128;   // 16-byte chunks of K, and of V, that a warp has in flight
 
+// kSeveral: p.tokens_at_once > 1.
+template <bool kSeveral>
 __global__ void __launch_bounds__(32 * kWriteWarps) cache_write_kernel(const CacheWriteParams p) {
   wait_for_previous_kernel();
   const int lane = threadIdx.x & 31;
-  const int token = blockIdx.x * kWriteWarps + (threadIdx.x >> 5);
-  if (token >= p.total) return;
-  const int chunks = p.cache.heads_kv * kRowChunks;
-  const uint16_t* k = p.k + token * p.k_token;
-  const uint16_t* v = p.v + token * p.v_token;
+  const int64_t begin = (static_cast<int64_t>(blockIdx.x) * kWriteWarps + (threadIdx.x >> 5)) * p.tokens_per_warp;
+  if (begin >= p.total) return;
+  const int first = static_cast<int>(begin), end = static_cast<int>(min(begin + p.tokens_per_warp, static_cast<int64_t>(p.total)));
+  const int token_chunks = p.cache.heads_kv * kRowChunks;
+  const int at_once = kSeveral ? p.tokens_at_once : 1;
   uint4 kx[4], vx[4];
-  auto load = [&](int first) {
+  // chunk c of the tokens from `token` on
+  auto load = [&](int token, int c0) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int c = first + 32 * i + lane;
-      if (c < chunks) {
-        kx[i] = __ldcs(reinterpret_cast<const uint4*>(k + (c / kRowChunks) * p.k_head + (c % kRowChunks) * 8));
-        vx[i] = __ldcs(reinterpret_cast<const uint4*>(v + (c / kRowChunks) * p.v_head + (c % kRowChunks) * 8));
+      const int c = c0 + 32 * i + lane, t = kSeveral ? c / token_chunks : 0, in_row = c - t * token_chunks;
+      if (kSeveral ? (t < at_once && token + t < end) : c < token_chunks) {
+        kx[i] = __ldcs(reinterpret_cast<const uint4*>(p.k + (token + t) * p.k_token + (in_row / kRowChunks) * p.k_head + (in_row % kRowChunks) * 8));
+        vx[i] = __ldcs(reinterpret_cast<const uint4*>(p.v + (token + t) * p.v_token + (in_row / kRowChunks) * p.v_head + (in_row % kRowChunks) * 8));
       }
     }
   };
-  load(0);
-  const int seq = last_not_above(p.cache.batch, token, [&](int b) { return __ldcg(p.cu + b); });
-  const int2 rows = sequence_rows(p.cu, seq, p.total, p.status, 6);
-  if (token < rows.x || token >= rows.y) return;   // behind the last sequence
-  const int place = max(__ldcg(p.cache.lens + seq), 0) - (rows.y - token);
-  const int page = page_of(p.cache, seq, place >> p.cache.page_shift, p.status, 7);
-  if (page < 0) return;
-  const int at = place & ((1 << p.cache.page_shift) - 1);
-  uint16_t* k_to = p.cache.k + page * p.cache.k_page + at * p.cache.k_place;
-  uint16_t* v_to = p.cache.v + page * p.cache.v_page + at * p.cache.v_place;
-  for (int first = 0;;) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int c = first + 32 * i + lane;
-      if (c < chunks) {
-        *reinterpret_cast<uint4*>(k_to + (c / kRowChunks) * p.cache.k_head + (c % kRowChunks) * 8) = kx[i];
-        *reinterpret_cast<uint4*>(v_to + (c / kRowChunks) * p.cache.v_head + (c % kRowChunks) * 8) = vx[i];
-      }
+  load(first, 0);
+  int seq = last_not_above(p.cache.batch, first, [&](int b) { return __ldcg(p.cu + b); });
+  int2 rows = sequence_rows(p.cu, seq, p.total, p.status, 6);
+  int len = max(__ldcg(p.cache.lens + seq), 0);
+  for (int token = first; token < end; token += at_once) {
+    // where lane t's token goes, token + t (of one token: every lane's)
+    const int mine = kSeveral ? min(token + min(lane, at_once - 1), end - 1) : token;
+    while (mine >= rows.y && seq + 1 < p.cache.batch) {
+      rows = sequence_rows(p.cu, ++seq, p.total, p.status, 6);
+      len = max(__ldcg(p.cache.lens + seq), 0);
     }
-    first += 128;
-    if (first >= chunks) break;
-    load(first);
+    int page = -1;
+    const int place = len - (rows.y - mine);
+    if (mine >= rows.x && mine < rows.y) page = page_of(p.cache, seq, place >> p.cache.page_shift, p.status, 7);   // (else behind the last sequence)
+    const int at = place & ((1 << p.cache.page_shift) - 1);
+    for (int c0 = 0;;) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = c0 + 32 * i + lane, t = kSeveral ? c / token_chunks : 0, in_row = c - t * token_chunks;
+        const int to_page = kSeveral ? __shfl_sync(0xffffffffu, page, t) : page, to = kSeveral ? __shfl_sync(0xffffffffu, at, t) : at;
+        if ((kSeveral ? (t < at_once && token + t < end) : c < token_chunks) && to_page >= 0) {
+          const int64_t head = in_row / kRowChunks, piece = (in_row % kRowChunks) * 8;
+          *reinterpret_cast<uint4*>(p.cache.k + to_page * p.cache.k_page + to * p.cache.k_place + head * p.cache.k_head + piece) = kx[i];
+          *reinterpret_cast<uint4*>(p.cache.v + to_page * p.cache.v_page + to * p.cache.v_place + head * p.cache.v_head + piece) = vx[i];
+        }
+      }
+      c0 += kWriteChunks;
+      if (kSeveral || c0 >= token_chunks) break;
+      load(token, c0);
+    }
+    if (token + at_once < end) load(token + at_once, 0);
   }
 }
 
@@ -399,9 +413,20 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictPar
 
 }  // namespace
 
-cudaError_t launch_cache_write(const CacheWriteParams& p, cudaStream_t stream) {
-  const int ctas = (p.total + kWriteWarps - 1) / kWriteWarps;
-  return launch_overlapped(cache_write_kernel, ctas, ctas, 32 * kWriteWarps, 0, stream, p);
+cudaError_t launch_cache_write(CacheWriteParams p, cudaStream_t stream) {
+  const int token_chunks = p.cache.heads_kv * kRowChunks;
+  p.tokens_at_once = token_chunks < kWriteChunks ? kWriteChunks / token_chunks : 1;
+  // A warp has a token's chunks in one turn (5 to 8 heads): then two tokens to a warp, so that the second one's loads are on their
+  // way while the first is written (one | two | four, us: 48,000 tokens of 8 heads 69.2 | 64.1 | 65.4, of 6 57.5 | 51.6 | 52.1, 16,000
+  // of 8 26.0 | 24.4 | 24.6), unless these are few. With more heads a token has turns enough (32 heads, prompts of 20,000: 107.3 |
+  // 109.9 | 111.4); with fewer, several tokens to a turn hide the way to their places (48,000 of 4 heads 38.9 | 41.0 | 42.0; a token
+  // to a turn, 4 heads 47.8 -> 38.9, 2 40.5 -> 21.4, 1 37.1 -> 10.7).
+  const bool one_turn = p.tokens_at_once == 1 && token_chunks <= kWriteChunks;
+  p.tokens_per_warp = one_turn && p.total >= 8192 ? 2 : p.tokens_at_once;
+  const int64_t warps = (static_cast<int64_t>(p.total) + p.tokens_per_warp - 1) / p.tokens_per_warp;
+  const int ctas = static_cast<int>((warps + kWriteWarps - 1) / kWriteWarps);
+  return p.tokens_at_once > 1 ? launch_overlapped(cache_write_kernel<true>, ctas, ctas, 32 * kWriteWarps, 0, stream, p)
+                              : launch_overlapped(cache_write_kernel<false>, ctas, ctas, 32 * kWriteWarps, 0, stream, p);
 }
 
 cudaError_t launch_cache_evict(const EvictParams& p, cudaStream_t stream) {

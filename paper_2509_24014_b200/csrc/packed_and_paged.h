@@ -54,9 +54,10 @@ struct CacheWriteParams {
   int64_t k_token, k_head, v_token, v_head;
   const int32_t* cu;       // [batch + 1]
   int total;
+  int tokens_at_once, tokens_per_warp;   // (launch_cache_write)
   DeviceStatus* status;
 };
-cudaError_t launch_cache_write(const CacheWriteParams& p, cudaStream_t stream);
+cudaError_t launch_cache_write(CacheWriteParams p, cudaStream_t stream);
 
 // One new token per sequence (attention_paged.cu). Workspace behind the status block, in this order: PagedLayout.
 struct PagedParams {

@@ -232,6 +232,26 @@ def test_rows_of_the_padded_batch_stay_empty():
     assert (o[2:] == 0).all() and (lse[2:] == -float("inf")).all() and o[:2].isfinite().all()
 
 
+@pytest.mark.parametrize("heads_kv", [1, 2, 3, 4, 5, 8, 9, 16])
+@pytest.mark.parametrize("lens", [[9000, 0, 1, 700], [3] * 400 + [0] * 3 + [1] * 50, [1], [7, 0, 0, 0, 9]])
+def test_write_tokens_per_warp(heads_kv, lens):
+    """One, two and several tokens to a warp, over sequences' ends and empty sequences, rows behind the last one left out."""
+    gen = su.generator(17)
+    lens_all = [n + (5 * i) % 40 for i, n in enumerate(lens)]
+    k, v, table = su.paged_pool(lens_all, 16, heads_kv, torch.bfloat16, gen)
+    want_k, want_v = k.clone(), v.clone()
+    n = sum(lens)
+    k_new, v_new = su.rows(n + 3, heads_kv, torch.bfloat16, gen, "fused"), su.rows(n + 3, heads_kv, torch.bfloat16, gen, "head")
+    ws = sd.new_workspace(256, "cuda")
+    sd.sparsed_cache_write(sd.make_cache(k, v, table, i32(lens_all)), k_new, v_new, su.offsets(lens), ws)
+    seq = np.repeat(np.arange(len(lens)), lens)
+    first = np.cumsum([0] + lens[:-1])
+    place = torch.from_numpy(np.array(lens_all)[seq] - np.array(lens)[seq] + np.arange(n) - first[seq]).cuda()
+    page = table[torch.from_numpy(seq).cuda(), place // 16].long()
+    want_k[page, place % 16], want_v[page, place % 16] = k_new[:n], v_new[:n]
+    assert torch.equal(k, want_k) and torch.equal(v, want_v) and su.status(ws) == (0, 0)
+
+
 def test_write_wide_rows_and_slices():
     """Heads enough that a warp takes a token's row in several turns; K and V as slices of one projection, a head-major pool."""
     heads, gen = 21, su.generator(13)
