@@ -1126,7 +1126,7 @@ extern "C" sparsed_status sparsed_cache_evict(const sparsed_cache* from, const f
   if (mass_capacity < room || mass_out_capacity < most) return SPARSED_ERR_INVALID_ARG;
   if (keep > (INT32_MAX >> 1)) return SPARSED_ERR_UNSUPPORTED;   // as the places of a cache
   const int64_t rows = static_cast<int64_t>(from->batch) * from->heads_kv;
-  if (rows * (keep / 32 + 1ll) > INT32_MAX / 2) return SPARSED_ERR_UNSUPPORTED;
+  if (rows * (keep / 8 + 1ll) > INT32_MAX / 2) return SPARSED_ERR_UNSUPPORTED;
   if (!aligned4(mass) || !aligned4(mass_out) || !aligned4(kept)) return SPARSED_ERR_ALIGNMENT;
   if ((st = check_ws(ws, ws_bytes, SPARSED_STATUS_BYTES)) != SPARSED_OK) return st;
   if (overlap(mass, rows * mass_capacity, mass_out, rows * mass_out_capacity)) return SPARSED_ERR_INVALID_ARG;

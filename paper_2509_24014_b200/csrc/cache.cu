@@ -361,52 +361,53 @@ __global__ void __launch_bounds__(kSelectThreads, 1024 / kSelectThreads) evict_s
 }
 
 // ------------------------------------------------------------------------------------------
-// Eviction, second half: the kept rows of K and V to their new pages. A warp moves 32 keys of a row: each lane looks up one
-// key's place and its new one, then sixteen lanes at a time move a key's 256 bytes, four keys of K and V in flight per lane.
-// Bound by HBM: whole calls move 2 x 16384 keys x 8 heads in 69.5 us (18 of them the selection, then 5.3 TB/s, read and written).
+// Eviction, second half: the kept rows of K and V to their new pages. A warp moves eight keys of a row: eight lanes look up one
+// key's place and its new one each, then sixteen lanes at a time move a key's 256 bytes, four keys of K and V in flight per lane.
+// Bound by HBM where there is much to move: 2 x 16384 keys x 8 heads, 268 MB read and written, in 43 us (6.2 TB/s); else by the
+// chain kept - page - data. (32 keys to a warp, the whole call, us: 2 rows of 30,000 18.6 against 16.0, 4 of 32,768 20.1 | 18.2, 2 of
+// 4000 12.6 | 9.9, 2 x 52k x 8 69.7 | 69.2; 128 of 2000 20.0 | 21.7.)
 // ------------------------------------------------------------------------------------------
 constexpr int kMoveThreads = 128;
+constexpr int kMoveKeys = 8;   // to a warp
 
 __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictParams p) {
   wait_for_previous_kernel();
   const int lane = threadIdx.x & 31, number = blockIdx.x * (kMoveThreads / 32) + (threadIdx.x >> 5);
-  const int warps_per_row = (p.keep + 31) / 32;
-  const int row = number / warps_per_row, j = (number - row * warps_per_row) * 32 + lane;
+  const int warps_per_row = (p.keep + kMoveKeys - 1) / kMoveKeys;
+  const int row = number / warps_per_row, j = (number - row * warps_per_row) * kMoveKeys + lane;
   if (row >= p.from.batch * p.from.heads_kv) return;
   const int seq = row / p.from.heads_kv, head = row - seq * p.from.heads_kv;
-  const int from = j < p.keep ? __ldcg(p.kept + static_cast<int64_t>(row) * p.keep + j) : -1;
+  const int from = lane < kMoveKeys && j < p.keep ? __ldcg(p.kept + static_cast<int64_t>(row) * p.keep + j) : -1;
   int page = -1, new_page = -1;
   if (from >= 0) {
     new_page = page_of(p.to, seq, j >> p.to.page_shift, p.status, 10);
     page = page_of(p.from, seq, from >> p.from.page_shift, p.status, 9);
   }
+  if (__all_sync(0xffffffffu, new_page < 0)) return;
   const int place = from & ((1 << p.from.page_shift) - 1), new_place = j & ((1 << p.to.page_shift) - 1);
   const int c = (lane & 15) * 8;
   const uint16_t* k = p.from.k + head * p.from.k_head + c;
   const uint16_t* v = p.from.v + head * p.from.v_head + c;
   uint16_t* new_k = p.to.k + head * p.to.k_head + c;
   uint16_t* new_v = p.to.v + head * p.to.v_head + c;
-  for (int i0 = 0; i0 < 32; i0 += 8) {
-    if (__all_sync(0xffffffffu, lane < i0 || new_page < 0)) break;
-    uint4 kx[4], vx[4];
+  uint4 kx[4], vx[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int key = i0 + 2 * i + (lane >> 4);
-      const int at_page = __shfl_sync(0xffffffffu, page, key), at = __shfl_sync(0xffffffffu, place, key);
-      kx[i] = vx[i] = make_uint4(0u, 0u, 0u, 0u);   // (a key whose page is missing comes over as zeros)
-      if (at_page >= 0) {
-        kx[i] = __ldcs(reinterpret_cast<const uint4*>(k + at_page * p.from.k_page + at * p.from.k_place));
-        vx[i] = __ldcs(reinterpret_cast<const uint4*>(v + at_page * p.from.v_page + at * p.from.v_place));
-      }
+  for (int i = 0; i < 4; ++i) {
+    const int key = 2 * i + (lane >> 4);
+    const int at_page = __shfl_sync(0xffffffffu, page, key), at = __shfl_sync(0xffffffffu, place, key);
+    kx[i] = vx[i] = make_uint4(0u, 0u, 0u, 0u);   // (a key whose page is missing comes over as zeros)
+    if (at_page >= 0) {
+      kx[i] = __ldcs(reinterpret_cast<const uint4*>(k + at_page * p.from.k_page + at * p.from.k_place));
+      vx[i] = __ldcs(reinterpret_cast<const uint4*>(v + at_page * p.from.v_page + at * p.from.v_place));
     }
+  }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int key = i0 + 2 * i + (lane >> 4);
-      const int to_page = __shfl_sync(0xffffffffu, new_page, key), to = __shfl_sync(0xffffffffu, new_place, key);
-      if (to_page >= 0) {
-        *reinterpret_cast<uint4*>(new_k + to_page * p.to.k_page + to * p.to.k_place) = kx[i];
-        *reinterpret_cast<uint4*>(new_v + to_page * p.to.v_page + to * p.to.v_place) = vx[i];
-      }
+  for (int i = 0; i < 4; ++i) {
+    const int key = 2 * i + (lane >> 4);
+    const int to_page = __shfl_sync(0xffffffffu, new_page, key), to = __shfl_sync(0xffffffffu, new_place, key);
+    if (to_page >= 0) {
+      *reinterpret_cast<uint4*>(new_k + to_page * p.to.k_page + to * p.to.k_place) = kx[i];
+      *reinterpret_cast<uint4*>(new_v + to_page * p.to.v_page + to * p.to.v_place) = vx[i];
     }
   }
 }
@@ -471,7 +472,7 @@ cudaError_t launch_cache_evict(const EvictParams& p, cudaStream_t stream) {
   e = cudaLaunchKernelEx(&cfg, variant.kernel, p);
   if (e == cudaSuccess) {
     cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>((static_cast<int64_t>((p.keep + 31) / 32) * rows + kMoveThreads / 32 - 1) / (kMoveThreads / 32)));
+    cfg.gridDim = dim3(static_cast<unsigned>((static_cast<int64_t>((p.keep + kMoveKeys - 1) / kMoveKeys) * rows + kMoveThreads / 32 - 1) / (kMoveThreads / 32)));
     cfg.blockDim = dim3(kMoveThreads);
     cfg.stream = stream;
     attr[0] = {};
