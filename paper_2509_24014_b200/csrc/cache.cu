@@ -433,8 +433,9 @@ cudaError_t launch_cache_write(CacheWriteParams p, cudaStream_t stream) {
 cudaError_t launch_cache_evict(const EvictParams& p, cudaStream_t stream) {
   const int rows = p.from.batch * p.from.heads_kv;
   // Several CTAs to a row that is long enough to be shared, as long as they take no more than 64 SMs: a CTA needs an SM for
-  // itself and a cluster the SMs of one part of the device, so more would not run at the same time. The whole call, us: 16 rows of
-  // 52k in clusters of 8 (two rounds) 74.1, of 4 69.5, of 2 87.0, one CTA to a row 120; 8 rows of 128k, 8 49.9, 4 49.9, 2 74.5,
+  // itself and a cluster the SMs of one part of the device, so more would not run at the same time. The whole call, us (this and
+  // the figures below with 32 keys to a moving warp, which adds 0.5 to 2): 16 rows of
+  // 52k in clusters of 8 (two rounds) 74.1, of 4 69.5, of 2 87.0, one CTA to a row 120; 8 rows of 128k, 8 or 4 49.9, 2 74.5,
   // one 123; 4 rows of 32k, 8 19.9, 4 20.2, 2 21.5. Of short rows a cluster's barriers and remote reads cost more than it gains:
   // 32 rows of up to 4k, one CTA 22.2, two 28.1; 16 rows of 8000, one 17.5, two 19.6, four 19.1; 8 of 16000, two 20.7, four 18.9.
   const int room = p.from.max_pages << p.from.page_shift;
