@@ -188,8 +188,10 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     const int key0 = tile * kUnit + warp * kWarpKeys;
     return tile < tile1 && key0 < len ? page_of(c, seq, key0 >> c.page_shift, p.status, 12) : -1;
   };
-  // K (0) or V (1) of this warp's keys in a unit on its way, by one lane, after all lanes have read what was there
+  // K (0) or V (1) of this warp's keys in a unit on its way, by one lane, after all lanes have read what was there. The reads are
+  // ordinary ones and the copy is not: without the fence, keys that are in L2 can land before the last of the reads is done.
   auto load = [&](int which, int tile, int at_page) {
+    fence_proxy_async_smem();
     __syncwarp();
     if (at_page >= 0 && lane == 0) {
       mbar_expect_tx(&sm.full[warp][which], kTileBytes);

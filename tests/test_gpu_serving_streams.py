@@ -205,6 +205,41 @@ def test_paged_many_query_heads_to_one_head():
     check_paged(su.rows(3, 71, torch.float16, gen), k, v, table, lens, with_mass=True)
 
 
+@pytest.mark.parametrize("lens,heads_q,heads_kv,page,dtype", [
+    ([117, 250, 318, 337, 404, 233, 122, 149, 95], 32, 32, 256, "bf16"), ([104, 98, 128, 112, 132, 91, 111] * 5, 32, 32, 16, "bf16"),
+    ([1060, 975, 1253, 1157, 869, 1047] * 9, 2, 2, 32, "fp16"), ([700, 33, 5000, 64], 28, 4, 64, "bf16"), ([300] * 30, 40, 2, 128, "fp16")])
+def test_paged_keys_that_are_in_l2(lens, heads_q, heads_kv, page, dtype):
+    """Keys and values that have just been written come back much sooner than ones from memory: the same bits, and no trace of the
+    unused places (NaN) around them."""
+    gen = su.generator(18)
+    k, v, table = su.paged_pool(lens, page, heads_kv, su.DTYPES[dtype], gen)
+    su.poison_unused(k, v, table, lens)
+    k0, v0 = k.clone(), v.clone()
+    q = su.rows(len(lens), heads_q, su.DTYPES[dtype], gen, scale=2.0)
+    cache = sd.make_cache(k, v, table, i32(lens))
+    ws = sd.new_workspace(sd.sparsed_paged_workspace_bytes(cache, heads_q, True), "cuda")
+    mass, o = torch.zeros(len(lens), heads_kv, table.shape[1] * page, device="cuda"), torch.empty_like(q)
+    flush = torch.empty(300 << 20, dtype=torch.uint8, device="cuda")
+
+    def call(warm):
+        mass.zero_()
+        if warm:
+            k.copy_(k0)
+            v.copy_(v0)
+        else:
+            flush.fill_(1)
+        sd.sparsed_attn_paged(q, cache, o, ws, mass_out=mass)
+        return o.clone(), mass.clone()
+
+    check_paged(q, k, v, table, lens, with_mass=True)
+    want_o, want_mass = call(False)
+    assert want_o.isfinite().all() and want_mass.isfinite().all()
+    for i in range(20):
+        got_o, got_mass = call(i % 4 != 3)
+        assert torch.equal(got_o, want_o) and torch.equal(got_mass, want_mass), i
+    assert su.status(ws) == (0, 0)
+
+
 def test_the_same_page_twice():
     lens, gen = [200, 130], su.generator(11)
     k, v, table = su.paged_pool(lens, 16, 2, torch.bfloat16, gen)
