@@ -17,16 +17,16 @@ OBJ_DIR = os.path.join(PKG_DIR, "build")
 LIB_PATH = os.path.join(PKG_DIR, "libsparsed.so")
 SOURCES = ["api.cu", "attention.cu", "attention_lone.cu", "attention_dense_pair.cu", "attention_dense_pair_split.cu",
            "scoring.cu", "topk.cu", "pool_select.cu", "patterns.cu", "pooled_qk.cu", "attention_packed.cu", "attention_packed_pair.cu",
-           "attention_paged.cu",
-           "cache.cu"]
+           "attention_paged.cu", "cache.cu"]
 HEADERS = ["internal.h", "dense_choice.h", "attention_dense_pair.cu", "sm100_primitives.cuh", "sm100_pair_primitives.cuh",
-           "softmax_pipeline.cuh", "work_items.cuh", "topk_device.cuh", "packed_and_paged.h", "packed_rows.cuh", "sequences.cuh", os.path.join("..", "..", "include", "sparsed.h")]
+           "softmax_pipeline.cuh", "work_items.cuh", "topk_device.cuh", "packed_and_paged.h", "packed_rows.cuh", "sequences.cuh",
+           os.path.join("..", "..", "include", "sparsed.h")]
 ARCH_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a"]
 COMMON_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC"]
 # Flags of single files. The CTA-pair dense kernel is built with denormals flushed to zero: its softmax handles
 # probabilities, for which a flushed 1e-38 is as good as the number, and the kernel measured 2-4 % faster that way
-# (8k-64k); what is multiplied into the outputs keeps them (mul_keep_denormals). The other kernels measured the same or
-# slower with it and keep IEEE denormals.
+# (8k-64k); what is multiplied into the outputs keeps them (mul_keep_denormals). So is
+# the packed kernel with the same pipeline. The other kernels measured the same or slower with it and keep IEEE denormals.
 PER_FILE_FLAGS = {"attention_dense_pair.cu": ["-ftz=true"], "attention_dense_pair_split.cu": ["-ftz=true"],
                   "attention_packed_pair.cu": ["-ftz=true"]}
 

@@ -20,7 +20,8 @@ namespace sparsed {
 // The 16-bit type of Q, K, V, P and O. (Most calls take bf16 only; the packed ones fp16 too.)
 // kSlack: how far (base 2) a row's sum over a tile may outgrow the reference in use before the reference is moved. P's relative
 // precision does not depend on it: with bf16 it is bounded by what P * V may reach in fp32 (2^24 leaves V 2^103), with fp16 by
-// P itself (2^16); what lies 2^-25 below the reference is 0 in fp16, which a sum over n keys may miss n * 2^-25 of V by. (Most calls' kernels move it from 2^8 on, which costs them little on the inputs they were measured with.)
+// P itself (2^16); what lies 2^-25 below the reference is 0 in fp16, which a sum over n keys may miss n * 2^-25 of V by.
+// (Most calls' kernels move it from 2^8 on, which costs them little on the inputs they were measured with.)
 struct Bf16Type {
   static constexpr float kSlack = 24.f;
   static constexpr uint32_t kExponents = 0x7f807f80u;     // exponent bits of a pair
