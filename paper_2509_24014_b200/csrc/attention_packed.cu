@@ -31,7 +31,7 @@
 // Bound: as the dense kernel, the tensor pipe and the softmax warps at the power limit (the device draws 1000 W and runs at 1.36
 // GHz in such calls); short sequences by what an item costs beside its tiles, about three tiles' worth. Measured, on visible
 // (row, key) pairs: 12 prompts of 165 to 3321 tokens, 28 heads on 4, some with cached text, causal, 0.79 T operations in 790 us (1.0
-// PFLOP/s); 8 sequences of 512 to 3980 tokens x 32 heads, no mask, fp16, 0.84 T in 885 us (0.95); six turns of 1 to 160 tokens x 8
+// PFLOP/s); 8 sequences of 512 to 3980 tokens x 32 heads, no mask, fp16, 0.84 T in 925 us (0.91); six turns of 1 to 160 tokens x 8
 // heads, 8.5 us in a graph. In-order taking of items leaves 2.5 % of either batch's time to its last items.
 // Not kept: four or six ring slots (2 % slower; no room), the next item fetched earlier (2 %), loads sent off before the barriers
 // are set up (short calls 0.2 us faster, 512 tokens 5 % slower), rows stored from tensor memory without the staging (7 %), a loop
@@ -359,17 +359,17 @@ attn_packed_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         bool exact = st.m == -INFINITY;   // nothing accumulated yet: no reference maximum to try
         if (!__any_sync(0xffffffffu, exact)) {
           sums = softmax_group_fast<Type>(r0, r1, scale_log2, st.m, pk);
-          exact = sums.x + sums.y > static_cast<float>(1u << static_cast<int>(Type::kSlack));   // logits outgrew the running maximum (a NaN makes the row NaN either way)
+          exact = sums.x + sums.y > Type::kMostSum;   // logits outgrew the running maximum (a NaN makes the row NaN either way)
         }
         if (__any_sync(0xffffffffu, exact)) {
-          // Rows whose reference has to move take their own maximum of the tile; the others keep theirs and get the same P
+          // Rows whose reference has to move take their own maximum of the tile, less the headroom; the others keep theirs and get the same P
           // again, so that a row's result does not depend on its neighbours (later tokens, with a causal mask).
           float alpha = 1.f;
           if (exact) {
             float top = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 32; ++j) top = fmaxf(top, fmaxf(__uint_as_float(r0[j]), __uint_as_float(r1[j])));
-            top *= scale_log2;
+            top = top * scale_log2 - Type::kHeadroom;
             if (top > st.m) {
               alpha = fast_exp2(st.m - top);   // 0 when nothing was accumulated yet
               st.m = top;

@@ -301,7 +301,7 @@ attn_packed_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
       bool exact = st.m == -INFINITY;   // nothing accumulated yet: no reference maximum to try
       if (!__any_sync(0xffffffffu, exact)) {
         sums = softmax_group_fast<Type>(r0, r1, scale_log2, st.m, pk);
-        exact = sums.x + sums.y > static_cast<float>(1u << static_cast<int>(Type::kSlack));
+        exact = sums.x + sums.y > Type::kMostSum;
       }
       if (__any_sync(0xffffffffu, exact)) {
         // (as in attention_packed.cu)
@@ -310,7 +310,7 @@ attn_packed_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
           float top = -INFINITY;
 #pragma unroll
           for (int j = 0; j < 32; ++j) top = fmaxf(top, fmaxf(__uint_as_float(r0[j]), __uint_as_float(r1[j])));
-          top *= scale_log2;
+          top = top * scale_log2 - Type::kHeadroom;
           if (top > st.m) {
             alpha = fast_exp2(st.m - top);   // 0 when nothing was accumulated yet
             st.m = top;

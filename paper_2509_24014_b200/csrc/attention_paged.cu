@@ -304,7 +304,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                 logits[(8 * n + (x & 1)) * room + key0 + 8 * (x >> 1)] = s[n][x];
         }
         if (__any_sync(0xffffffffu, outgrown)) {
-          // logits well above their head's reference (or there is none yet): the tile's maximum becomes the reference
+          // logits well above their head's reference (or there is none yet): the tile's maximum, less the headroom, becomes the reference
 #pragma unroll
           for (int n = 0; n < kNT; ++n)
 #pragma unroll
@@ -314,6 +314,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
               if (top > m[n][x] + Type::kSlack) {   // (a head's result does not depend on the other heads)
+                top -= Type::kHeadroom;
                 const float alpha = fast_exp2(m[n][x] - top);   // 0 when nothing was accumulated yet
                 m[n][x] = top;
                 l[n][x] *= alpha;

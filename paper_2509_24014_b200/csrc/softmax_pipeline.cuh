@@ -20,10 +20,16 @@ namespace sparsed {
 // The 16-bit type of Q, K, V, P and O. (Most calls take bf16 only; the packed ones fp16 too.)
 // kSlack: how far (base 2) a row's sum over a tile may outgrow the reference in use before the reference is moved. P's relative
 // precision does not depend on it: with bf16 it is bounded by what P * V may reach in fp32 (2^24 leaves V 2^103), with fp16 by
-// P itself (2^16); what lies 2^-25 below the reference is 0 in fp16, which a sum over n keys may miss n * 2^-25 of V by.
+// P itself (65504). kMostSum: 2^kSlack.
 // (Most calls' kernels move it from 2^8 on, which costs them little on the inputs they were measured with.)
+// kHeadroom: how far below the largest logit (base 2) the reference is put when it moves. fp16 has its full precision down to
+// 2^-14 of the reference, and nothing at all from 2^-25 down: with the reference at the largest logit, one key of 0.98 of the
+// weight (a sink, whose V may be 0) took up to all of what the others give. 2^8 below it, weights from 2^-22 of the largest up
+// are rounded by half a step, smaller ones by 2^-33 of the largest at most; and 64 keys at the largest logit do not yet move it.
+// (It moves more often for that: 8 sequences of 512 to 3980 tokens x 32 heads, no mask, keys of which one in 64 has much weight,
+// 848 -> 885 us, with a slack of 2^15 914; one-token calls take as long as before.)
 struct Bf16Type {
-  static constexpr float kSlack = 24.f;
+  static constexpr float kSlack = 24.f, kMostSum = 16777216.f, kHeadroom = 0.f;
   static constexpr uint32_t kExponents = 0x7f807f80u;     // exponent bits of a pair
   static constexpr uint32_t kExponentCarry = 0x00800080u; // added to them: bit 15 / 31 is set where all were ones
   static __host__ __device__ constexpr uint32_t idesc(uint32_t bf16) { return bf16; }
@@ -33,7 +39,7 @@ struct Bf16Type {
   }
 };
 struct Fp16Type {
-  static constexpr float kSlack = 15.f;
+  static constexpr float kSlack = 15.98f, kMostSum = 64624.f, kHeadroom = 8.f;
   static constexpr uint32_t kExponents = 0x7c007c00u;
   static constexpr uint32_t kExponentCarry = 0x04000400u;
   static __host__ __device__ constexpr uint32_t idesc(uint32_t bf16) { return bf16 & ~((1u << 7) | (1u << 10)); }   // both formats 0: fp16
