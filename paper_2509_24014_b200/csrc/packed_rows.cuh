@@ -41,14 +41,17 @@ __device__ __forceinline__ int2 packed_tile_and_head(const PackedParams& p, int 
   return make_int2(p.tiles - 1 - in_pass / heads_here, pass * p.heads_per_pass + in_pass % heads_here);
 }
 
-// Whether this thread's row of a 64-column half of a V tile (128 bytes a row) holds an infinity or NaN.
+// Whether this thread's row of a 64-column half of a V tile (128 bytes a row) holds an infinity or NaN. (Volatile, as the writes
+// of clean_half_row: in the CTA-pair kernel two threads look at a row, and either may clean it.)
 template <class Type>
 __device__ __forceinline__ bool has_non_finite(const uint16_t* half_tile, int row) {
-  const uint4* chunks = reinterpret_cast<const uint4*>(half_tile + row * 64);
+  const uint32_t chunks = smem_u32(half_tile + row * 64);
   uint32_t found = 0;
 #pragma unroll
   for (int c = 0; c < 8; ++c) {
-    const uint4 x = chunks[(c + row) & 7];   // (rotated: rows are 128 bytes apart; the swizzle does not matter here)
+    uint4 x;   // (rotated: rows are 128 bytes apart; the swizzle does not matter here)
+    asm volatile("ld.volatile.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(chunks + ((c + row) & 7) * 16) : "memory");
     found |= non_finite_pair<Type>(x.x) | non_finite_pair<Type>(x.y) | non_finite_pair<Type>(x.z) | non_finite_pair<Type>(x.w);
   }
   return found != 0u;
@@ -57,11 +60,10 @@ __device__ __forceinline__ bool has_non_finite(const uint16_t* half_tile, int ro
 // Makes it zero there.
 template <class Type>
 __device__ __forceinline__ void clean_half_row(uint16_t* half_tile, int row) {
-  uint32_t* words = reinterpret_cast<uint32_t*>(half_tile + row * 64);
+  volatile uint32_t* words = reinterpret_cast<volatile uint32_t*>(half_tile + row * 64);
   for (int i = 0; i < 32; ++i) {
-    const uint32_t bad = non_finite_pair<Type>(words[i]);
-    if (bad & 0x8000u) words[i] &= 0xffff0000u;
-    if (bad & 0x80000000u) words[i] &= 0x0000ffffu;
+    const uint32_t x = words[i], bad = non_finite_pair<Type>(x);
+    if (bad != 0u) words[i] = x & ((bad & 0x8000u ? 0xffff0000u : ~0u) & (bad & 0x80000000u ? 0x0000ffffu : ~0u));
   }
 }
 
