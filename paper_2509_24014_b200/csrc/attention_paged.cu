@@ -33,6 +33,7 @@
 // and after the stream of keys: lengths - page - first tiles, about 3 us, and the joining kernel, 4 to 8.
 #include <algorithm>
 
+#include "paged_loads.h"
 #include "sequences.cuh"
 #include "softmax_pipeline.cuh"
 
@@ -235,6 +236,14 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 
   begin_segment();
   bool ok = true;
+  // A wait has run out: what this warp has on its way must have landed before the CTA leaves (bounded like every wait).
+  auto drain = [&](PagedWait failed) {
+    const PagedLoads loads = paged_loads_on_their_way(failed, uses, next_page >= 0);
+    for (uint32_t i = 0; loads.keys && i < kSpinLimit && !mbar_try_wait(&sm.full[warp][0], loads.keys_use & 1); ++i) {
+    }
+    for (uint32_t i = 0; loads.values && i < kSpinLimit && !mbar_try_wait(&sm.full[warp][1], loads.values_use & 1); ++i) {
+    }
+  };
   while (true) {
     float o[kNT][8][4];
     float m[kNT][2], l[kNT][2];
@@ -259,7 +268,10 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         float s[kNT][4];
         {
           ok = mbar_wait(&sm.full[warp][0], uses & 1, &sm.abort_flag, p.status, 15);
-          if (!(ok = __all_sync(0xffffffffu, ok))) break;
+          if (!(ok = __all_sync(0xffffffffu, ok))) {
+            drain(PagedWait::kKeys);
+            break;
+          }
           uint32_t kx[2][16];   // rows g and g + 8, pieces 4 i + t
           const uint32_t at = k_tile + spread * 128 + ((t ^ spread) << 4);
 #pragma unroll
@@ -341,7 +353,10 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         }
         // ---- O^T += V^T P^T. Rows 2t, 2t + 1, 2t + 8, 2t + 9 of S^T are keys t, t + 4, t + 8, t + 12.
         ok = mbar_wait(&sm.full[warp][1], uses & 1, &sm.abort_flag, p.status, 16);
-        if (!(ok = __all_sync(0xffffffffu, ok))) break;
+        if (!(ok = __all_sync(0xffffffffu, ok))) {
+          drain(PagedWait::kValues);
+          break;
+        }
         uint32_t vx[4][8];   // pieces `spread` and `spread` + 8 of the four keys
         const uint32_t at = v_tile + t * 128 + ((spread ^ t) << 4);
 #pragma unroll
@@ -444,10 +459,6 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     // (the shares are read before any warp writes the next segment's: two barriers lie between)
     if (unit >= unit1) return;
   }
-  // Given up: what is on its way must have landed before the CTA leaves (bounded like every wait).
-  for (int which = 0; which < 2; ++which)
-    for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(&sm.full[warp][which], uses & 1); ++i) {
-    }
 }
 
 // ------------------------------------------------------------------------------------------
