@@ -362,7 +362,7 @@ sparsed_status sparsed_cache_write(const sparsed_cache *cache, const void *k_new
  * device fp32 [batch, heads_q], natural log. An empty sequence gets zeros and -inf.
  * mass_out_or_null: device fp32 [batch, heads_kv, mass_capacity], mass_capacity >= max_pages * page_size: receives, for
  * j < seq_lens[b], mass_in[b,g,j] (0 without mass_in) + the sum of p_hj over the query heads h of key-value head g; what lies
- * behind a sequence's length is left as it was. mass_in may be mass_out itself. The work is divided over the device by the
+ * behind a sequence's length is left as it was. mass_in may be mass_out itself, but must not overlap it otherwise. The work is divided over the device by the
  * lengths found in seq_lens, so a sequence's result may differ in its last bits with what else is in the batch; the same
  * inputs give the same bits. seq_lens and the table are read on the device while the call runs (a captured call takes those of
  * the moment it is replayed) and must not change meanwhile. P is rounded to the 16-bit type as in sparsed_attn_packed, each part of

@@ -1069,6 +1069,10 @@ extern "C" sparsed_status sparsed_attn_paged(const sparsed_cache* cache, int32_t
   if (with_mass && mass_capacity < static_cast<int64_t>(cache->max_pages) * cache->page_size) return SPARSED_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(o) || !aligned4(lse_or_null) || !aligned4(mass_in_or_null) || !aligned4(mass_out_or_null))
     return SPARSED_ERR_ALIGNMENT;
+  // (each weight is read by the thread that writes it, in no order: the same array or another)
+  const int64_t masses = static_cast<int64_t>(cache->batch) * cache->heads_kv * mass_capacity;
+  if (mass_in_or_null != nullptr && mass_in_or_null != mass_out_or_null && overlap(mass_in_or_null, masses, mass_out_or_null, masses))
+    return SPARSED_ERR_INVALID_ARG;
   const int group = heads_q / cache->heads_kv;
   const PagedLayout at = paged_layout(cache->batch, cache->heads_kv, group, cache->max_pages, cache->page_size, with_mass);
   if ((st = check_ws(ws, ws_bytes, static_cast<size_t>(at.bytes))) != SPARSED_OK) return st;
