@@ -310,8 +310,9 @@ sparsed_status sparsed_pattern_validate(const sparsed_pattern *pattern, void *ws
  * The same inputs give the same bits, whatever else is in the batch, except that a sequence's bits may depend on which of two
  * kernels takes the call. That goes by num_seqs, total_q, total_k, heads and the mask; SPARSED_PACKED_KERNEL=single or =pair in
  * the environment (read once) makes it one of them for all calls. P is rounded to the 16-bit type against a reference that lies
- * below a row's largest logit, by up to 24 powers of two in bf16 (|V| beyond 2^103 may overflow) and by 8 to 16 in fp16 (weights
- * below 2^-22 of a row's largest are off by up to 2^-33 of that, larger ones by half a step of the type).
+ * below a row's largest logit, by up to 24 powers of two in bf16 (so |V| beyond 2^103 / n, with n keys to a row, may overflow the
+ * fp32 sums) and by 8 to 16 in fp16 (weights below 2^-22 of a row's largest are off by up to 2^-33 of that, larger ones by half a
+ * step of the type).
  * The workspace holds the status only, so calls that overlap may share it: SPARSED_STATUS_BYTES. Errors: INVALID_ARG, UNSUPPORTED (head_dim != 128, dtype), ALIGNMENT, WORKSPACE, ARCH, CUDA.
  */
 typedef struct sparsed_packed {
@@ -365,8 +366,8 @@ sparsed_status sparsed_cache_write(const sparsed_cache *cache, const void *k_new
  * behind a sequence's length is left as it was. mass_in may be mass_out itself, but must not overlap it otherwise. The work is divided over the device by the
  * lengths found in seq_lens, so a sequence's result may differ in its last bits with what else is in the batch; the same
  * inputs give the same bits. seq_lens and the table are read on the device while the call runs (a captured call takes those of
- * the moment it is replayed) and must not change meanwhile. P is rounded to the 16-bit type as in sparsed_attn_packed, each part of
- * a sequence against its own largest logits; the sums and the weights in mass_out take it unrounded.
+ * the moment it is replayed) and must not change meanwhile. P is rounded to the 16-bit type as in sparsed_attn_packed (with the
+ * same bound on |V|), each part of a sequence against its own largest logits; the sums and the weights in mass_out take it unrounded.
  * Workspace: sparsed_paged_workspace_bytes(cache, heads_q, with_mass) bytes (with_mass: mass_out is given). It holds parts of
  * results: calls that may overlap (on two streams, in two graphs) need a workspace each; calls in one stream may share one. At most
  * 4096 query heads to a key-value head.

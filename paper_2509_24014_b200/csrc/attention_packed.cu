@@ -24,9 +24,10 @@
 // finite becomes 0 there, and where it belongs to a key of this sequence, which some rows of the tile see, it is added to
 // those rows' outputs in the epilogue, element by element.
 //
-// Roundings: logits, softmax sums and O are fp32. P goes to the tensor cores in the inputs' 16-bit type, half a step of it per
-// weight (2^-9 in bf16, 2^-12 in fp16) with either sign, while the sum takes it unrounded; O is rounded once, at the end. Errors
-// against 64 bits, of O's size: bf16 2.2e-3, fp16 2.9e-4, where rounding an exact O alone gives 1.7e-3 and 2.1e-4.
+// Roundings: logits, softmax sums and O are fp32. P goes to the tensor cores in the inputs' 16-bit type, which the MMA wants for both
+// operands: up to half a step of it per weight (2^-8 of the weight in bf16, 2^-11 in fp16), with either sign, while the sum takes
+// it unrounded; O is rounded once, at the end. Errors against 64 bits, of O's size: bf16 2.2e-3, fp16 2.9e-4, where rounding an
+// exact O alone gives 1.7e-3 and 2.1e-4.
 //
 // Bound: as the dense kernel, the tensor pipe and the softmax warps at the power limit (the device draws 1000 W and runs at 1.36
 // GHz in such calls); short sequences by what an item costs beside its tiles, about three tiles' worth. Measured, on visible

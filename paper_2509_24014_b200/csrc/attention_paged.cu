@@ -25,7 +25,7 @@
 // key against 512 per key), from which p = 2^(logit - LSE) follows once the LSE is known.
 //
 // Roundings: logits, sums, O and weights are fp32 throughout. P goes to the matrix instructions in the cache's 16-bit type, the
-// sum of a softmax takes it unrounded: half a step of P, 2^-9 of a weight in bf16 and 2^-12 in fp16, with either sign, averages
+// sum of a softmax takes it unrounded: up to half a step of P, 2^-8 of a weight in bf16 and 2^-11 in fp16, with either sign, averages
 // out over the keys (errors against 64 bits 2.3e-3 of O's size in bf16, most of it O's own rounding, 2.9e-4 in fp16).
 //
 // Measured (caches cold): 24 x 6000-8192 keys x 32 heads 416 us, 6.7 TB/s; 131072 x 8 heads 90, 5.9; 48 x 300-8000 x 4 heads

@@ -19,8 +19,8 @@ namespace sparsed {
 
 // The 16-bit type of Q, K, V, P and O. (Most calls take bf16 only; the packed ones fp16 too.)
 // kSlack: how far (base 2) a row's sum over a tile may outgrow the reference in use before the reference is moved. P's relative
-// precision does not depend on it: with bf16 it is bounded by what P * V may reach in fp32 (2^24 leaves V 2^103), with fp16 by
-// P itself (65504). kMostSum: 2^kSlack.
+// precision does not depend on it: with bf16 it is bounded by what the sum of P * V over a row's n keys may reach in fp32 (n * 2^24
+// leaves |V| 2^103 / n), with fp16 by P itself (65504). kMostSum: 2^kSlack.
 // (Most calls' kernels move it from 2^8 on, which costs them little on the inputs they were measured with.)
 // kHeadroom: how far below the largest logit (base 2) the reference is put when it moves. fp16 has its full precision down to
 // 2^-14 of the reference, and nothing at all from 2^-25 down: with the reference at the largest logit, one key of 0.98 of the
