@@ -19,7 +19,7 @@ SOURCES = ["api.cu", "attention.cu", "attention_lone.cu", "attention_dense_pair.
            "scoring.cu", "topk.cu", "pool_select.cu", "patterns.cu", "pooled_qk.cu", "attention_packed.cu", "attention_packed_pair.cu",
            "attention_paged.cu", "cache.cu"]
 HEADERS = ["internal.h", "dense_choice.h", "attention_dense_pair.cu", "sm100_primitives.cuh", "sm100_pair_primitives.cuh",
-           "softmax_pipeline.cuh", "work_items.cuh", "topk_device.cuh", "packed_and_paged.h", "packed_rows.cuh", "sequences.cuh", "paged_loads.h",
+           "softmax_pipeline.cuh", "work_items.cuh", "topk_device.cuh", "packed_and_paged.h", "packed_rows.cuh", "sequences.cuh", "paged_loads.h", "cache_choice.h",
            os.path.join("..", "..", "include", "sparsed.h")]
 ARCH_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a"]
 COMMON_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC"]

@@ -3,6 +3,7 @@
 // length -> page table -> data) where there is little to move.
 #include <cooperative_groups.h>
 
+#include "cache_choice.h"
 #include "sequences.cuh"
 #include "topk_device.cuh"
 
@@ -89,8 +90,6 @@ __global__ void __launch_bounds__(32 * kWriteWarps) cache_write_kernel(const Cac
 // cold caches) the loads take 2.7, a step 0.5 for counting, 0.25 for adding up and 0.2 for the bin, the writing 2.2; of 18 us for
 // 13,000 in each of four CTAs 5, 3 and 7.
 // ------------------------------------------------------------------------------------------
-constexpr int kMostRanks = 8;    // CTAs to a row
-constexpr int kShortRow = 2048;  // the most keys of a row that a CTA of 256 threads takes
 constexpr int kBins = 2048;
 constexpr int kScanThreads = 256;   // that add up and scan the bins (with all 1024 the instructions of it took twice as long)
 constexpr int kLoadBatch = 4;    // weights that a thread has on their way when a CTA reads its run
@@ -432,19 +431,6 @@ cudaError_t launch_cache_write(CacheWriteParams p, cudaStream_t stream) {
 
 cudaError_t launch_cache_evict(const EvictParams& p, cudaStream_t stream) {
   const int rows = p.from.batch * p.from.heads_kv;
-  // Several CTAs to a row that is long enough to be shared, as long as they take no more than 64 SMs: a CTA needs an SM for
-  // itself and a cluster the SMs of one part of the device, so more would not run at the same time. The whole call, us (this and
-  // the figures below with 32 keys to a moving warp, which adds 0.5 to 2): 16 rows of
-  // 52k in clusters of 8 (two rounds) 74.1, of 4 69.5, of 2 87.0, one CTA to a row 120; 8 rows of 128k, 8 or 4 49.9, 2 74.5,
-  // one 123; 4 rows of 32k, 8 19.9, 4 20.2, 2 21.5. Of short rows a cluster's barriers and remote reads cost more than it gains:
-  // 32 rows of up to 4k, one CTA 22.2, two 28.1; 16 rows of 8000, one 17.5, two 19.6, four 19.1; 8 of 16000, two 20.7, four 18.9.
-  const int room = p.from.max_pages << p.from.page_shift;
-  int ranks = 1;
-  while (ranks < kMostRanks && rows * ranks * 2 <= 64 && room / (2 * ranks) >= 2048) ranks *= 2;
-  // Short rows get CTAs of 256 threads, four to an SM: the call with 1024 | 256 threads, us, 352 rows of up to 59 keys 22.2 | 14.0,
-  // 148 of 1000 23.2 | 20.4, 32 of 1000 12.3 | 11.6, 4 of 1000 10.9 | 10.3, 128 of 2000 22.5 | 19.9; but 32 of 2000 13.3 | 13.7 and
-  // 256 of 4000 41.6 | 43.3.
-  const bool short_rows = room <= (rows > 64 ? kShortRow : kShortRow / 2);
   struct Variant {
     void (*kernel)(EvictParams);
     int threads, smem;
@@ -452,7 +438,8 @@ cudaError_t launch_cache_evict(const EvictParams& p, cudaStream_t stream) {
   constexpr Variant variants[5] = {{evict_select_kernel<1, 1024>, 1024, sizeof(EvictSmem<1, 1024>)}, {evict_select_kernel<2, 1024>, 1024, sizeof(EvictSmem<2, 1024>)},
                                    {evict_select_kernel<4, 1024>, 1024, sizeof(EvictSmem<4, 1024>)}, {evict_select_kernel<8, 1024>, 1024, sizeof(EvictSmem<8, 1024>)},
                                    {evict_select_kernel<1, 256>, 256, sizeof(EvictSmem<1, 256>)}};
-  const int which = ranks > 1 ? (ranks == 2 ? 1 : (ranks == 4 ? 2 : 3)) : (short_rows ? 4 : 0);
+  const EvictChoice choice = choose_evict_variant(rows, p.from.max_pages << p.from.page_shift);
+  const int ranks = choice.ranks, which = ranks > 1 ? (ranks == 2 ? 1 : (ranks == 4 ? 2 : 3)) : (choice.threads == 256 ? 4 : 0);
   const Variant& variant = variants[which];
   static SmemLimit limits[5];
   cudaError_t e = ensure_dynamic_smem(variant.kernel, variant.smem, limits[which]);
