@@ -11,7 +11,7 @@
 //     most ten tiles of 64 keys can be masked for 512 tokens, and the ring has ten slots for V.)
 //   * rows go out from the staged tile with ordinary stores: the tile at a sequence's end must not touch the next sequence.
 // When a call comes here: packed_pair_pays (dense_choice.h). Roundings as there. Bound by the power limit: 32768 tokens x 32 heads,
-// causal, 8.8 T operations in 7.0 ms (1.26 PFLOP/s; the single-CTA kernel 7.6), 2 x 8192 x 32 heads without a mask 1.81 ms
+// causal, 8.8 T operations in 7.0 to 7.1 ms (1.24 PFLOP/s; the single-CTA kernel 7.5), 2 x 8192 x 32 heads without a mask 1.81 ms
 // (1.21; 1.97).
 #include <type_traits>
 

@@ -1,7 +1,7 @@
 // Attention of one new token per sequence over a paged key-value cache, head_dim 128, bf16 or fp16, fp32 softmax.
 //
-// Every cached key and value is read once and used for the few query heads of its group only, so HBM bounds it: what matters
-// is that every SM keeps loads in flight all the time, whatever the lengths are. A warp takes 16 keys at a time: one TMA
+// Every cached key and value is read once (with more than 16 query heads in a group once for every 16 of them) and used for these few
+// heads only, so HBM bounds it: what matters is that every SM keeps loads in flight all the time, whatever the lengths are. A warp takes 16 keys at a time: one TMA
 // instruction brings their K (4 KB), one their V, each into a place that only this warp reads, and the next one is issued as
 // soon as the warp has the current one in registers. 16 warps an SM, 128 KB on their way. (Measured on this pattern alone, 2.8
 // GB: TMA 6.9 TB/s with 64 to 192 KB on their way, 16-byte loads into registers 6.8, cp.async 5.2. As loads into registers
@@ -29,8 +29,9 @@
 // out over the keys (errors against 64 bits 2.3e-3 of O's size in bf16, most of it O's own rounding, 2.9e-4 in fp16).
 //
 // Measured (caches cold): 24 x 6000-8192 keys x 32 heads 416 us, 6.7 TB/s; 131072 x 8 heads 90, 5.9; 48 x 300-8000 x 4 heads
-// 53, 4.4 (with weights 57); one sequence of 1500 keys x 4 heads 7.5 in a graph. The shorter ones are bound by what comes before
-// and after the stream of keys: lengths - page - first tiles, about 3 us, and the joining kernel, 4 to 8.
+// 53, 4.4 (with weights 57); one sequence of 1500 keys x 4 heads 7.5 in a graph; 131072 x 2 heads with 32 query heads 37, with 40,
+// which are two walks over 134 MB, 46. The shorter ones are bound by what comes before and after the stream of keys: lengths - page -
+// first tiles, about 3 us, and the joining kernel, 4 to 8.
 #include <algorithm>
 
 #include "paged_loads.h"

@@ -82,7 +82,10 @@ inline DenseKernel choose_dense_kernel(bool with_stats, long long bh, int seq_le
 }
 
 // Whether attention over packed sequences goes to the kernel whose MMAs span CTA pairs (attention_packed_pair.cu): four tiles of
-// `tile_tokens` tokens to a cluster. The lengths are only known on the device, so this goes by their averages.
+// `tile_tokens` tokens to a cluster. The lengths are only known on the device, so this goes by their averages over the rows of the
+// buffers, and a captured call keeps its choice. What that costs where the averages say little, 32 heads, us, pair | single: one
+// sequence of 32768 rows and 31 of none, causal (taken for 1024 each: single) 6904 | 7504; in buffers of 32768 rows (taken for full
+// ones: pair) 2 sequences of 300, causal, 93 | 67, 2 of 1000 124 | 91, 8 of 300 without a mask 128 | 89.
 // Beside the keys that rows see (`keys`, on average), a cluster pays for its set-up, about 200 keys' worth, and with a causal mask
 // for the keys that only its last tokens see, half of its tokens on average, where a CTA of the other kernel pays for half of a
 // tile's. Per key it takes 0.905 of the other's time under sustained load (0.91 after a rest). Measured, pair over single, after
