@@ -307,14 +307,15 @@ sparsed_status sparsed_pattern_validate(const sparsed_pattern *pattern, void *ws
  * Offsets that descend or leave [0, total] are clipped, never followed, and recorded as device status 6. The rows of o (and of
  * lse) must not overlap one another or the inputs. cu_q and cu_k are read on the device while the call runs, so a captured call
  * takes the lengths of the moment it is replayed; they must not change while it runs.
- * The same inputs give the same bits, whatever else is in the batch, except that a sequence's bits may depend on which of two
- * kernels takes the call. That goes by num_seqs, total_q, total_k, heads and the mask, so by the averages of the buffers' rows and not by
- * the lengths in them: sequences of no rows that fill a batch up, or many rows behind the last sequence, can bring the slower kernel
- * (a 32k sequence among 31 empty ones takes 9 % longer, 300 tokens in a buffer for 32k 40 %), and a captured call keeps its kernel.
- * SPARSED_PACKED_KERNEL=single or =pair in the environment (read once) makes it one of them for all calls. P is rounded to the 16-bit type against a reference that lies
- * below a row's largest logit, by up to 24 powers of two in bf16 (so |V| beyond 2^103 / n, with n keys to a row, may overflow the
- * fp32 sums) and by 8 to 16 in fp16 (weights below 2^-22 of a row's largest are off by up to 2^-33 of that, larger ones by half a
- * step of the type; in bf16 what is below 2^-100 of the largest may be lost).
+ * The same inputs give the same bits, whatever else is in the batch, except that a sequence's bits may depend on which of
+ * two kernels takes the call. That goes by num_seqs, total_q, total_k, heads and the mask, so by the averages of the
+ * buffers' rows and not by the lengths in them: sequences of no rows that fill a batch up, or many rows behind the last
+ * sequence, can bring the slower kernel (a 32k sequence among 31 empty ones takes 9 % longer, 300 tokens in a buffer for 32k
+ * 40 %), and a captured call keeps its kernel. SPARSED_PACKED_KERNEL=single or =pair in the environment (read once) makes it
+ * one of them for all calls. P is rounded to the 16-bit type against a reference that lies below a row's largest logit, by
+ * up to 24 powers of two in bf16 (so |V| beyond 2^103 / n, with n keys to a row, may overflow the fp32 sums) and by 8 to 16
+ * in fp16 (weights below 2^-22 of a row's largest are off by up to 2^-33 of that, larger ones by half a step of the type; in
+ * bf16 what is below 2^-100 of the largest may be lost).
  * The workspace holds the status only, so calls that overlap may share it: SPARSED_STATUS_BYTES. Errors: INVALID_ARG, UNSUPPORTED (head_dim != 128, dtype), ALIGNMENT, WORKSPACE, ARCH, CUDA.
  */
 typedef struct sparsed_packed {
@@ -363,19 +364,19 @@ sparsed_status sparsed_cache_write(const sparsed_cache *cache, const void *k_new
  *   o[b,h] = sum_j p_hj V_j, j < seq_lens[b], p_h = softmax(softmax_scale * q[b,h] K^T).
  * q, o: device [batch, heads_q, 128] of the cache's type, strides (sequence, head), all-zero = contiguous. lse_or_null:
  * device fp32 [batch, heads_q], natural log. An empty sequence gets zeros and -inf.
- * mass_out_or_null: device fp32 [batch, heads_kv, mass_capacity], mass_capacity >= max_pages * page_size: receives, for
- * j < seq_lens[b], mass_in[b,g,j] (0 without mass_in) + the sum of p_hj over the query heads h of key-value head g; what lies
- * behind a sequence's length is left as it was. mass_in may be mass_out itself, but must not overlap it otherwise. The work is divided over the device by the
- * lengths found in seq_lens, so a sequence's result may differ in its last bits with what else is in the batch; the same
- * inputs give the same bits. seq_lens and the table are read on the device while the call runs (a captured call takes those of
- * the moment it is replayed) and must not change meanwhile. P is rounded to the 16-bit type as in sparsed_attn_packed (with the
- * same bound on |V|), each part of a sequence against its own largest logits; the sums and the weights in mass_out take it unrounded.
- * o, lse and mass_out must not overlap one another or the inputs (but for mass_in). Each key and value is read once for every 16 query heads
- * of its group, once in all for up to 16.
- * Workspace: sparsed_paged_workspace_bytes(cache, heads_q, with_mass) bytes (with_mass: mass_out is given; then it has 4 bytes for
- * every query head and place of the page table, however short the sequences are). It holds parts of
- * results: calls that may overlap (on two streams, in two graphs) need a workspace each; calls in one stream may share one. At most
- * 4096 query heads to a key-value head.
+ * mass_out_or_null: device fp32 [batch, heads_kv, mass_capacity], mass_capacity >= max_pages * page_size: receives, for j <
+ * seq_lens[b], mass_in[b,g,j] (0 without mass_in) + the sum of p_hj over the query heads h of key-value head g; what lies
+ * behind a sequence's length is left as it was. mass_in may be mass_out itself, but must not overlap it otherwise. The work
+ * is divided over the device by the lengths found in seq_lens, so a sequence's result may differ in its last bits with what
+ * else is in the batch; the same inputs give the same bits. seq_lens and the table are read on the device while the call
+ * runs (a captured call takes those of the moment it is replayed) and must not change meanwhile. P is rounded to the 16-bit
+ * type as in sparsed_attn_packed (with the same bound on |V|), each part of a sequence against its own largest logits; the
+ * sums and the weights in mass_out take it unrounded. o, lse and mass_out must not overlap one another or the inputs (but
+ * for mass_in). Each key and value is read once for every 16 query heads of its group, once in all for up to 16.
+ * Workspace: sparsed_paged_workspace_bytes(cache, heads_q, with_mass) bytes (with_mass: mass_out is given; then it has 4
+ * bytes for every query head and place of the page table, however short the sequences are). It holds parts of results: calls
+ * that may overlap (on two streams, in two graphs) need a workspace each; calls in one stream may share one. At most 4096
+ * query heads to a key-value head.
  */
 sparsed_status sparsed_paged_workspace_bytes(const sparsed_cache *cache, int32_t heads_q, int32_t with_mass,
                                              size_t *out_bytes); /* host only */

@@ -29,12 +29,13 @@
 // it unrounded; O is rounded once, at the end. Errors against 64 bits, of O's size: bf16 2.2e-3, fp16 2.9e-4, where rounding an
 // exact O alone gives 1.7e-3 and 2.1e-4.
 //
-// Bound: as the dense kernel, the tensor pipe and the softmax warps at the power limit (the device draws 1000 W and runs at 1.36
-// GHz in such calls); a launch by itself, with the clock at its highest, takes 0.88 of that time with tensor pipe and exponential
-// unit busy 60 to 63 % each, the rest being the latency of a tile's steps and of the first and last items; short sequences by what an item costs beside its tiles, about three tiles' worth. Measured, on visible
-// (row, key) pairs: 12 prompts of 165 to 3321 tokens, 28 heads on 4, some with cached text, causal, 0.79 T operations in 790 us (1.0
-// PFLOP/s); 8 sequences of 512 to 3980 tokens x 32 heads, no mask, fp16, 0.84 T in 885 to 917 us (0.93); six turns of 1 to 160 tokens x 8
-// heads, 8.5 us in a graph. In-order taking of items leaves 2.5 % of either batch's time to its last items.
+// Bound: as the dense kernel, the tensor pipe and the softmax warps at the power limit (the device draws 1000 W and runs at
+// 1.36 GHz in such calls); a launch by itself, with the clock at its highest, takes 0.88 of that time with tensor pipe and
+// exponential unit busy 60 to 63 % each, the rest being the latency of a tile's steps and of the first and last items; short
+// sequences by what an item costs beside its tiles, about three tiles' worth. Measured, on visible (row, key) pairs: 12 prompts
+// of 165 to 3321 tokens, 28 heads on 4, some with cached text, causal, 0.79 T operations in 790 us (1.0 PFLOP/s); 8 sequences
+// of 512 to 3980 tokens x 32 heads, no mask, fp16, 0.84 T in 885 to 917 us (0.93); six turns of 1 to 160 tokens x 8 heads, 8.5
+// us in a graph. In-order taking of items leaves 2.5 % of either batch's time to its last items.
 // Not kept: four or six ring slots (2 % slower; no room), the next item fetched earlier (2 %), loads sent off before the barriers
 // are set up (short calls 0.2 us faster, 512 tokens 5 % slower), rows stored from tensor memory without the staging (7 %), a loop
 // of two open tiles (spills, 10 %).

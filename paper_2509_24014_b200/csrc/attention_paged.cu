@@ -1,11 +1,12 @@
 // Attention of one new token per sequence over a paged key-value cache, head_dim 128, bf16 or fp16, fp32 softmax.
 //
-// Every cached key and value is read once (with more than 16 query heads in a group once for every 16 of them) and used for these few
-// heads only, so HBM bounds it: what matters is that every SM keeps loads in flight all the time, whatever the lengths are. A warp takes 16 keys at a time: one TMA
-// instruction brings their K (4 KB), one their V, each into a place that only this warp reads, and the next one is issued as
-// soon as the warp has the current one in registers. 16 warps an SM, 128 KB on their way. (Measured on this pattern alone, 2.8
-// GB: TMA 6.9 TB/s with 64 to 192 KB on their way, 16-byte loads into registers 6.8, cp.async 5.2. As loads into registers
-// the whole kernel took 436 us for 24 x 7000 keys x 32 heads, its accumulators leaving no room for the tiles.)
+// Every cached key and value is read once (with more than 16 query heads in a group once for every 16 of them) and used for
+// these few heads only, so HBM bounds it: what matters is that every SM keeps loads in flight all the time, whatever the
+// lengths are. A warp takes 16 keys at a time: one TMA instruction brings their K (4 KB), one their V, each into a place
+// that only this warp reads, and the next one is issued as soon as the warp has the current one in registers. 16 warps an
+// SM, 128 KB on their way. (Measured on this pattern alone, 2.8 GB: TMA 6.9 TB/s with 64 to 192 KB on their way, 16-byte
+// loads into registers 6.8, cp.async 5.2. As loads into registers the whole kernel took 436 us for 24 x 7000 keys x 32
+// heads, its accumulators leaving no room for the tiles.)
 //   S^T [16 keys x 8 heads]  = K [16 x 128] Q^T: mma.m16n8k16 with K as the A operand. A dot product does not care in which
 //     order it takes head_dim, so a thread's A fragments of two k-steps are one 16-byte piece of a key row, and Q is read with
 //     the same permutation.

@@ -5,7 +5,7 @@ namespace sparsed {
 
 // Whether the last wave of `clusters` clusters over `pairs` SM pairs runs as clusters of one stream each. Such a
 // cluster takes 0.65-0.8 of the time of one with two. So a last wave that would leave half of the SM pairs idle or
-// more is launched that way: 16 x 3072 (1.3 waves) 95.0 -> 84.4 us (statistics recorded). So is a grid of less than half
+// more is launched that way: 16 heads in 1.3 waves 95.0 -> 84.4 us (statistics recorded). So is a grid of less than half
 // a wave, but only those of fewer than 256 keys come here (choose_dense_kernel). From two full waves on it gained nothing
 // (32 x 4096, 3.46 waves): there the launch is at the power limit, and an emptier last wave raises the clock (1755 MHz
 // against 1687 at 37 x 4096, 4.0 waves), which leaves 5 % of its cost (979 against 1029 TFLOP/s).
@@ -109,8 +109,8 @@ inline bool packed_pair_pays(long long num_seqs, long long total_q, long long to
 // 5.85 -> 5.56, six 12.3 -> 10.5; 16 x 512 block 32 (walked as the union of four rows' lists) one 7.72 -> 7.15, ten 11.9
 // -> 10.4; 2 x 4096 block 32, twelve 21.8 -> 16.3; no blocks at all, 8 x 1024 block 32, 4.2 -> 3.7; one whole row among
 // rows of one block, 2 x 8192 block 64, 91 -> 71. Side by side (alone | a pair): block 128, 72 items x 128 keys 0.98 | 0.98,
-// 80 x 256 0.95 | 1.09, x 512 0.93 | 1.05, 128 x 1024 0.86 | 1.18, x 2048 0.82 | 1.13, 148 x 2048 0.81 | 1.25, x 3072 0.79 |
-// 1.17; block 64 and 32, whose unions are longer than the lists, 100 x 128 0.90 | 1.10, 128 x 256 0.88 | 1.18 and 0.84 |
+// 80 x 256 0.95 | 1.09, x 512 0.93 | 1.05, 128 x 1024 0.86 | 1.18, x 2048 0.82 | 1.13, 148 x 2048 0.81 | 1.25;
+// block 64 and 32, whose unions are longer than the lists, 100 x 128 0.90 | 1.10, 128 x 256 0.88 | 1.18 and 0.84 |
 // 1.09, 144 x 512 0.82 | 1.14 and 0.83 | 1.12. keys: on average in the `rows` lists, as far as `nnz` (all entries) says;
 // 0 if it does not.
 inline bool sparse_lone_ctas_pay(long long items, long long nnz, long long rows, int num_blocks, int block_size,

@@ -39,7 +39,7 @@ struct Bf16Type {
   }
 };
 struct Fp16Type {
-  static constexpr float kSlack = 15.98f, kMostSum = 64624.f, kHeadroom = 8.f;
+  static constexpr float kSlack = 15.98f, kMostSum = 64633.f, kHeadroom = 8.f;
   static constexpr uint32_t kExponents = 0x7c007c00u;
   static constexpr uint32_t kExponentCarry = 0x04000400u;
   static __host__ __device__ constexpr uint32_t idesc(uint32_t bf16) { return bf16 & ~((1u << 7) | (1u << 10)); }   // both formats 0: fp16
